@@ -268,6 +268,131 @@ int64_t pb_plan_summary(const pb_net_desc* net, char* buf, int64_t cap);
 int pb_scale_hyperparameters(float lr_ref, float momentum_ref, int32_t n_ref, int32_t n, float* lr_out,
                              float* momentum_out);
 
+/* ---- Operators over plain device arrays -----------------------------------
+ * What a model of tokens needs around its matrix products, beside
+ * pb_update_standalone: the lookup of embeddings and its gradient, the log
+ * probabilities of given tokens and their gradient, and an AdamW step over all
+ * of its tensors.  All array arguments are DEVICE pointers; structures, lists
+ * of them and lists of sizes are host memory that is read before the call
+ * returns.  Calls are asynchronous on `stream` (a hipStream_t, NULL = the null
+ * stream), whose device must be the current one and hold the arrays; arrays
+ * last used on another stream are the caller's to order.  They allocate
+ * nothing and keep nothing: a captured call repeats its arguments, and two
+ * calls that may run at once need workspaces of their own.  Arguments are
+ * checked before anything is launched (PB_E_INVALID); a call with nothing to do
+ * (no tensor, row or token) succeeds.  Sums are held in 32 bits or more and do
+ * not depend on the order in which workgroups run: the same call gives the
+ * same bits. */
+typedef enum { PB_F32 = 0, PB_BF16 = 1 } pb_dtype;
+
+/* AdamW.  For each element, with the gradient g times *grad_scale where that
+ * is given, t = the step's number, from 1 on:
+ *   m <- beta1 m + (1 - beta1) g          v <- beta2 v + (1 - beta2) g^2
+ *   d  = (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *   w <- w - lr weight_decay w - lr d     w_hat = w - horizon lr d
+ * w_hat, where given, holds the weights as they will be after `horizon` more
+ * steps of the same d (the prediction w - lr T v of the pipeline, with Adam's
+ * direction for the velocity); horizon = 0: a copy of w in the type of w_hat.
+ *
+ * The moments of all tensors lie in two flat arrays of pb_adamw_elements
+ * entries, tensor i from the sum of the sizes before it on, each rounded up to
+ * PB_ADAMW_BLOCK.  moment_bits = 32: floats.  moment_bits = 8: one byte each,
+ * and one byte of exponent per PB_ADAMW_BLOCK entries in m_exp and v_exp.  Such
+ * a value is an fp32 number cut to 3 bits behind its leading one: with
+ * e = the exponent field of the block's largest magnitude (one more where that
+ * would round up to it), code c of v stands for the float with the bit pattern
+ * (c + 8 (e - 31)) << 20, the low seven bits c of m's code for
+ * (c + 8 (e - 15)) << 20 with the code's top bit as sign; c = 0, or a pattern
+ * that is not positive, stands for 0.  v reaches 2^-31 of its block's maximum
+ * and is never rounded to 0 (a weight whose v were 0 would take a step of
+ * m / eps), m reaches 2^-15.  Rounding is stochastic, up with the probability
+ * of the part that is cut off, by 16 bits for each of m and v from a splitmix64
+ * stream of (seed, t, the element's place in the flat arrays): rounding to
+ * nearest would hold v fast, since one step with beta2 = 0.999 moves it by far
+ * less than half a code.  The step itself uses the moments before they are
+ * rounded.  A block that takes in a value that is not finite (or of 1.875 *
+ * 2^127 and more) gets exponent 255 and reads as NaN from then on.  All zero
+ * bytes are moments of zero: where training starts. */
+enum { PB_ADAMW_BLOCK = 128 };
+
+typedef struct {
+  void* w;              /* n weights of type w_type, updated in place                   */
+  const void* g;        /* n gradients of type g_type                                   */
+  void* w_hat;          /* n predicted weights of type w_hat_type, written; or NULL     */
+  int64_t n;            /* any size; 0: the tensor is passed over                       */
+  double weight_decay;
+} pb_adamw_tensor;
+
+typedef struct {
+  int32_t w_type, g_type, w_hat_type;   /* pb_dtype, the same for all tensors of a call */
+  int32_t moment_bits;                  /* 32 or 8                                      */
+  double lr, beta1, beta2, eps;         /* lr, eps >= 0; 0 <= beta < 1                  */
+  double horizon;
+  int64_t step;                         /* t >= 1; not looked at where step_dev is given */
+  const int64_t* step_dev;              /* t in device memory, read when the step runs (a captured step counts on); or NULL */
+  const float* grad_scale;              /* one float in device memory (a clipping factor, 1 / loss scale); or NULL */
+  uint64_t seed;                        /* moment_bits = 8                              */
+} pb_adamw_desc;
+
+/* Entries of the flat moment arrays for tensors of n[0..n_tensors-1] elements. */
+int64_t pb_adamw_elements(const int64_t* n, int32_t n_tensors);
+
+/* m, v (and m_exp, v_exp where moment_bits = 8; NULL otherwise) on 16-byte boundaries; the tensors
+ * on boundaries of their element size (16 bytes is faster).  Entries between two tensors: 8-bit ones
+ * are written as 0, 32-bit ones left as they are.  step_dev counting from values below 1 gives NaN. */
+int pb_adamw_step(const pb_adamw_tensor* tensors, int32_t n_tensors, const pb_adamw_desc* desc, void* m, void* v,
+                  uint8_t* m_exp, uint8_t* v_exp, void* stream);
+
+/* What 8-bit moments stand for, as floats: n entries (a multiple of PB_ADAMW_BLOCK) of m into m_out and of v
+ * into v_out, both on 16-byte boundaries. */
+int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n,
+                     float* m_out, float* v_out, void* stream);
+
+/* Log probabilities.  For each row of `rows` rows of `vocab` logits (type `dtype`, rows row_stride elements
+ * apart), x = scale * logit (infinite beyond the range of 32 bits), M = max x, s = sum e^(x - M):
+ *   logp = x[target] - M - ln s           the target's log probability
+ *   entropy = ln s - sum (x - M) e^(x - M) / s
+ *   norm = (M, ln s)                      what the gradient takes
+ *   top_ids, top_logp [rows][top]         the `top` largest logits in falling order, of equal ones the lower
+ *                                         index first, and their log probabilities
+ * targets and top_ids are of id_bits (32 or 64) bits.  A target outside [0, vocab) marks a row that has none:
+ * its logp is 0.  A row whose logits are all -inf has no distribution: M = -inf, ln s = 0, entropy 0, the log
+ * probability of each token -inf.  A NaN, or +inf, makes the row's results NaN; a NaN counts as the largest logit in
+ * the order of the alternatives.  entropy may be NULL; targets and logp both NULL: no token is given.
+ * 0 < scale (one over a temperature), 0 <= top <= min(vocab, PB_TOP_MAX), vocab < 2^31, row_stride >= vocab.
+ * `workspace`: pb_log_probs_workspace bytes (NULL where that is 0), 16-byte aligned, free for other use when the
+ * call's work is done. */
+enum { PB_TOP_MAX = 64 };
+int64_t pb_log_probs_workspace(int64_t rows, int64_t vocab, int32_t top);
+int pb_log_probs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride, const void* targets,
+                 int32_t id_bits, float scale, float* logp, float* entropy, float* norm, int32_t top, float* top_logp,
+                 void* top_ids, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradient of sum_r g_logp[r] logp[r] + g_entropy[r] entropy[r] with respect to the logits, with ln p = x - M - ln s:
+ *   dlogits[j] = scale ( g_logp ([j = target] - p_j) - g_entropy p_j (ln p_j + entropy) )
+ * in the type of the logits, rounded once; rows d_stride elements apart.  norm, entropy: what pb_log_probs wrote
+ * for these logits.  g_logp NULL (then targets are not looked at) or g_entropy NULL (then entropy is not): no such term.
+ * A row without a target has no first term; a row whose logits are all -inf has a gradient of 0.  dlogits may be the logits' own array,
+ * if d_stride = row_stride, and must not overlap it otherwise. */
+int pb_log_probs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                          const void* targets, int32_t id_bits, float scale, const float* norm, const float* entropy,
+                          const float* g_logp, const float* g_entropy, void* dlogits, int64_t d_stride, void* stream);
+
+/* Embeddings.  out[i] = scale * table[ids[i]], rounded once to out_dtype: n rows of dim elements, one after the
+ * other, from a table of vocab rows.  An id outside [0, vocab) (padding) gives a row of zeros. */
+int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const void* ids, int32_t id_bits, int64_t n,
+             float scale, void* out, int32_t out_dtype, void* stream);
+
+/* Gradient of the table: for each row, scale * the sum of the rows of d_out (n rows of dim, type `dtype`) whose
+ * id is that row's, added up in 32 bits in the order of their places.  add = 0: d_table (vocab rows of dim, type
+ * table_dtype) is written, with zeros in rows that no id names; add = 1: the sums are added to it, and rows that no
+ * id names are left alone.  n <= 2^30, vocab <= 2^31.  `workspace`: pb_embed_backward_workspace bytes, 16-byte
+ * aligned, free for other use when the call's work is done. */
+int64_t pb_embed_backward_workspace(int64_t n, int64_t vocab, int64_t dim);
+int pb_embed_backward(const void* d_out, int32_t dtype, const void* ids, int32_t id_bits, int64_t n, int64_t vocab,
+                      int64_t dim, float scale, void* d_table, int32_t table_dtype, int32_t add, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
 int pb_sync(pb_ctx* ctx);
 void pb_destroy(pb_ctx* ctx);
 const char* pb_last_error(void);

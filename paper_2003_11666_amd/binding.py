@@ -16,7 +16,8 @@ OP_KIND = {"linear": 0, "conv": 1, "gn": 2, "relu": 3, "maxpool": 4, "gap": 5, "
 EXPORTS = ["pb_arena_bytes", "pb_init", "pb_init_static", "pb_static_arena_bytes", "pb_tick", "pb_run_resident", "pb_read_weights",
            "pb_read_velocity", "pb_loss_history", "pb_num_params", "pb_num_ticks",
            "pb_set_launch_mode", "pb_plan_summary", "pb_profile_begin", "pb_profile_end", "pb_update_standalone",
-           "pb_scale_hyperparameters",
+           "pb_scale_hyperparameters", "pb_adamw_elements", "pb_adamw_step", "pb_adamw_moments", "pb_log_probs_workspace",
+           "pb_log_probs", "pb_log_probs_backward", "pb_embed", "pb_embed_backward_workspace", "pb_embed_backward",
            "pb_sync", "pb_destroy", "pb_last_error"]
 
 

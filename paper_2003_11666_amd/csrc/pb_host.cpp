@@ -23,24 +23,25 @@
 #include "../../include/pb.h"
 #include "pb_device.h"
 #include "pb_mlp.h"
+#include "pb_ops.h"
 
 using namespace pb;
 
-namespace {
+static thread_local char g_err[512];   // (fixed: reporting a failure must not need memory)
 
-thread_local char g_err[512];   // (fixed: reporting a failure must not need memory)
-
-// contexts built by pb_init_static share one static device array per GPU: one at a time
-constexpr int MAX_STATIC_DEVS = 64;
-std::atomic<bool> g_static_busy[MAX_STATIC_DEVS] = {};
-
-int fail(int code, const char* fmt, ...) {
+int pb::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof g_err, fmt, ap);
   va_end(ap);
   return code;
 }
+
+namespace {
+
+// contexts built by pb_init_static share one static device array per GPU: one at a time
+constexpr int MAX_STATIC_DEVS = 64;
+std::atomic<bool> g_static_busy[MAX_STATIC_DEVS] = {};
 
 // Body of a C entry: no exception (host memory that ran out, in practice) leaves it.
 template <class R, class F>

@@ -1,0 +1,194 @@
+// C entries of the operators over plain device arrays (include/pb.h): arguments are checked here, before anything is launched.
+#include <math.h>
+
+#include "pb_ops.h"
+
+using namespace pb;
+
+namespace {
+
+int launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? (int)PB_OK : fail(PB_E_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+}
+
+bool is_type(int t) { return t == PB_F32 || t == PB_BF16; }
+size_t size_of(int t) { return t == PB_BF16 ? 2 : 4; }
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+
+constexpr int64_t MOST = (int64_t)1 << 42;   // elements of an array: products of sizes below stay within 63 bits
+
+int64_t in_blocks(int64_t n) { return (n + PB_ADAMW_BLOCK - 1) / PB_ADAMW_BLOCK; }
+
+// rows of `width` elements, `pitch` apart
+bool is_matrix(int64_t rows, int64_t width, int64_t pitch) { return rows >= 0 && width > 0 && pitch >= width && pitch <= MOST && (rows == 0 || rows <= MOST / pitch); }
+
+int bad_ids(const char* what, const void* ids, int id_bits) {
+  if (id_bits != 32 && id_bits != 64) return fail(PB_E_INVALID, "%s must be of 32 or 64 bits, not %d", what, (int)id_bits);
+  if (!aligned(ids, id_bits / 8)) return fail(PB_E_INVALID, "%s must lie on boundaries of their size", what);
+  return PB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t pb_adamw_elements(const int64_t* n, int32_t n_tensors) {
+  if (n_tensors < 0 || (n_tensors > 0 && !n)) return fail(PB_E_INVALID, "no sizes");
+  int64_t blocks = 0;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    if (n[i] < 0 || n[i] > MOST || (blocks += in_blocks(n[i])) > MOST / PB_ADAMW_BLOCK) return fail(PB_E_INVALID, "tensor %d: bad size", (int)i);
+  }
+  return blocks * PB_ADAMW_BLOCK;
+}
+
+int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_desc* d, void* m, void* v, uint8_t* m_exp, uint8_t* v_exp,
+                  void* stream) {
+  if (!d || n_tensors < 0 || (n_tensors > 0 && !ts)) return fail(PB_E_INVALID, "NULL argument");
+  if (!is_type(d->w_type) || !is_type(d->g_type) || !is_type(d->w_hat_type)) return fail(PB_E_INVALID, "types must be PB_F32 or PB_BF16");
+  if (d->moment_bits != 32 && d->moment_bits != 8) return fail(PB_E_INVALID, "moment_bits must be 32 or 8, not %d", (int)d->moment_bits);
+  if (!(d->lr >= 0) || !isfinite(d->lr) || !isfinite(d->horizon)) return fail(PB_E_INVALID, "lr must be >= 0, lr and horizon finite");
+  if (!(d->beta1 >= 0 && (float)d->beta1 < 1) || !(d->beta2 >= 0 && (float)d->beta2 < 1)) return fail(PB_E_INVALID, "betas must be in [0, 1)");
+  if (!((float)d->eps > 0) || !isfinite(d->eps)) return fail(PB_E_INVALID, "eps must be positive (as a 32-bit number)");
+  if (!d->step_dev && d->step < 1) return fail(PB_E_INVALID, "steps are counted from 1");
+  if (!aligned(d->step_dev, 8) || !aligned(d->grad_scale, 4)) return fail(PB_E_INVALID, "step_dev and grad_scale must lie on boundaries of their size");
+  int64_t blocks = 0, work = 0;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const pb_adamw_tensor& t = ts[i];
+    if (t.n < 0 || t.n > MOST || (blocks += in_blocks(t.n)) > MOST / PB_ADAMW_BLOCK) return fail(PB_E_INVALID, "tensor %d: bad size", (int)i);
+    if (t.n == 0) continue;
+    ++work;
+    if (!t.w || !t.g) return fail(PB_E_INVALID, "tensor %d: no weights or no gradient", (int)i);
+    if (!isfinite(t.weight_decay)) return fail(PB_E_INVALID, "tensor %d: weight_decay must be finite", (int)i);
+    if (!aligned(t.w, size_of(d->w_type)) || !aligned(t.g, size_of(d->g_type)) || !aligned(t.w_hat, size_of(d->w_hat_type)))
+      return fail(PB_E_INVALID, "tensor %d: arrays must lie on boundaries of their element size", (int)i);
+  }
+  if (!work) return PB_OK;
+  if (!m || !v || !aligned(m, 16) || !aligned(v, 16)) return fail(PB_E_INVALID, "m and v must be given, on 16-byte boundaries");
+  if (d->moment_bits == 8 ? !m_exp || !v_exp : m_exp || v_exp)
+    return fail(PB_E_INVALID, "m_exp and v_exp belong to 8-bit moments, and those to them");
+
+  AdamWArgs a = {};
+  a.b1 = (float)d->beta1; a.c1 = (float)(1.0 - d->beta1);
+  a.b2 = (float)d->beta2; a.c2 = (float)(1.0 - d->beta2);
+  a.eps = (float)d->eps; a.horizon = (float)d->horizon;
+  a.lr = d->lr; a.beta1 = d->beta1; a.beta2 = d->beta2;
+  a.step = d->step; a.step_dev = d->step_dev; a.grad_scale = d->grad_scale; a.seed = d->seed;
+  a.m = m; a.v = v; a.m_exp = m_exp; a.v_exp = v_exp;
+  int64_t at = 0, groups = 0;
+  auto launch = [&] {
+    launch_adamw(a, groups, d->w_type, d->g_type, d->w_hat_type, d->moment_bits, (hipStream_t)stream);
+    a.n_tensors = 0;
+    groups = 0;
+    return launched();
+  };
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const pb_adamw_tensor& t = ts[i];
+    if (t.n == 0) continue;
+    const int64_t g = (t.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+    if (g > 0x7fffffff) return fail(PB_E_INVALID, "tensor %d is too large", (int)i);
+    if (a.n_tensors == ADAMW_TENSORS || groups + g > 0x7fffffff) {
+      const int rc = launch();
+      if (rc) return rc;
+    }
+    const int k = a.n_tensors++;
+    a.w[k] = t.w; a.g[k] = t.g; a.hat[k] = t.w_hat; a.n[k] = t.n; a.at[k] = at;
+    a.first[k] = (int32_t)groups;
+    a.decay[k] = (float)(d->lr * t.weight_decay);
+    at += in_blocks(t.n) * PB_ADAMW_BLOCK;
+    groups += g;
+  }
+  return launch();
+}
+
+int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, void* stream) {
+  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
+  if (n == 0) return PB_OK;
+  if (!m || !v || !m_exp || !v_exp || !m_out || !v_out) return fail(PB_E_INVALID, "NULL argument");
+  if (((uintptr_t)m | (uintptr_t)v | (uintptr_t)m_out | (uintptr_t)v_out) % 16) return fail(PB_E_INVALID, "arrays must be 16-byte aligned");
+  launch_adamw_moments(m, v, m_exp, v_exp, n, m_out, v_out, (hipStream_t)stream);
+  return launched();
+}
+
+int64_t pb_log_probs_workspace(int64_t rows, int64_t vocab, int32_t top) {
+  if (!is_matrix(rows, vocab, vocab) || vocab > 0x7fffffff || top < 0 || top > PB_TOP_MAX || top > vocab) return fail(PB_E_INVALID, "bad sizes");
+  return logp_workspace(rows, vocab, top);
+}
+
+int pb_log_probs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride, const void* targets, int32_t id_bits, float scale,
+                 float* logp, float* entropy, float* norm, int32_t top, float* top_logp, void* top_ids, void* workspace, int64_t workspace_bytes,
+                 void* stream) {
+  if (!is_type(dtype)) return fail(PB_E_INVALID, "dtype must be PB_F32 or PB_BF16");
+  if (!is_matrix(rows, vocab, row_stride) || vocab > 0x7fffffff) return fail(PB_E_INVALID, "bad sizes: %lld rows of %lld logits, %lld apart", (long long)rows, (long long)vocab, (long long)row_stride);
+  if (rows > 0x7fffffff) return fail(PB_E_INVALID, "too many rows");
+  if (!(scale > 0) || !isfinite(scale)) return fail(PB_E_INVALID, "scale must be positive and finite");
+  if (top < 0 || top > PB_TOP_MAX || top > vocab) return fail(PB_E_INVALID, "top must be in [0, min(vocab, %d)]", (int)PB_TOP_MAX);
+  if (const int rc = bad_ids("targets and top_ids", targets, id_bits)) return rc;
+  if (rows == 0) return PB_OK;
+  if (!logits || !norm) return fail(PB_E_INVALID, "no logits or no norm");
+  if (!targets != !logp) return fail(PB_E_INVALID, "targets and logp belong together");
+  if (top > 0 && (!top_logp || !top_ids)) return fail(PB_E_INVALID, "top > 0 needs top_logp and top_ids");
+  if (!aligned(logits, size_of(dtype)) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(norm, 4) || (top > 0 && (!aligned(top_logp, 4) || !aligned(top_ids, id_bits / 8))))
+    return fail(PB_E_INVALID, "arrays must lie on boundaries of their element size");
+  const int64_t need = logp_workspace(rows, vocab, top);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
+    return fail(PB_E_INVALID, "workspace: %lld bytes on a 16-byte boundary are needed", (long long)need);
+  launch_logp({logits, rows, vocab, row_stride, targets, scale, logp, entropy, norm, top, top_logp, top_ids, workspace}, dtype, id_bits, (hipStream_t)stream);
+  return launched();
+}
+
+int pb_log_probs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride, const void* targets, int32_t id_bits,
+                          float scale, const float* norm, const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
+                          int64_t d_stride, void* stream) {
+  if (!is_type(dtype)) return fail(PB_E_INVALID, "dtype must be PB_F32 or PB_BF16");
+  if (!is_matrix(rows, vocab, row_stride) || !is_matrix(rows, vocab, d_stride) || vocab > 0x7fffffff || rows > 0x7fffffff)
+    return fail(PB_E_INVALID, "bad sizes: %lld rows of %lld logits, %lld and %lld apart", (long long)rows, (long long)vocab, (long long)row_stride, (long long)d_stride);
+  if (!(scale > 0) || !isfinite(scale)) return fail(PB_E_INVALID, "scale must be positive and finite");
+  if (const int rc = bad_ids("targets", targets, id_bits)) return rc;
+  if (rows == 0) return PB_OK;
+  if (!logits || !norm || !dlogits) return fail(PB_E_INVALID, "NULL argument");
+  if (g_logp && !targets) return fail(PB_E_INVALID, "g_logp needs targets");
+  if (g_entropy && !entropy) return fail(PB_E_INVALID, "g_entropy needs entropy");
+  if (!aligned(logits, size_of(dtype)) || !aligned(dlogits, size_of(dtype)) || (((uintptr_t)norm | (uintptr_t)entropy | (uintptr_t)g_logp | (uintptr_t)g_entropy) & 3))
+    return fail(PB_E_INVALID, "arrays must lie on boundaries of their element size");
+  const uintptr_t x0 = (uintptr_t)logits, x1 = x0 + size_of(dtype) * ((rows - 1) * row_stride + vocab);
+  const uintptr_t d0 = (uintptr_t)dlogits, d1 = d0 + size_of(dtype) * ((rows - 1) * d_stride + vocab);
+  if (x0 < d1 && d0 < x1 && !(x0 == d0 && row_stride == d_stride)) return fail(PB_E_INVALID, "dlogits overlaps the logits");
+  launch_logp_grad({logits, rows, vocab, row_stride, targets, scale, norm, entropy, g_logp, g_entropy, dlogits, d_stride}, dtype, id_bits, (hipStream_t)stream);
+  return launched();
+}
+
+int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const void* ids, int32_t id_bits, int64_t n, float scale, void* out,
+             int32_t out_dtype, void* stream) {
+  if (!is_type(dtype) || !is_type(out_dtype)) return fail(PB_E_INVALID, "types must be PB_F32 or PB_BF16");
+  if (vocab <= 0 || !is_matrix(vocab, dim, dim) || !is_matrix(n, dim, dim)) return fail(PB_E_INVALID, "bad sizes: a table of %lld rows of %lld, %lld ids", (long long)vocab, (long long)dim, (long long)n);
+  if (const int rc = bad_ids("ids", ids, id_bits)) return rc;
+  if (n == 0) return PB_OK;
+  if (!table || !ids || !out) return fail(PB_E_INVALID, "NULL argument");
+  if (!aligned(table, size_of(dtype)) || !aligned(out, size_of(out_dtype))) return fail(PB_E_INVALID, "arrays must lie on boundaries of their element size");
+  launch_embed({table, vocab, dim, n, ids, scale, out}, dtype, out_dtype, id_bits, (hipStream_t)stream);
+  return launched();
+}
+
+int64_t pb_embed_backward_workspace(int64_t n, int64_t vocab, int64_t dim) {
+  if (vocab <= 0 || vocab > (int64_t)1 << 31 || n > (int64_t)1 << 30 || !is_matrix(vocab, dim, dim) || !is_matrix(n, dim, dim)) return fail(PB_E_INVALID, "bad sizes");
+  return embed_grad_workspace(n, vocab, dim);
+}
+
+int pb_embed_backward(const void* d_out, int32_t dtype, const void* ids, int32_t id_bits, int64_t n, int64_t vocab, int64_t dim, float scale,
+                      void* d_table, int32_t table_dtype, int32_t add, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!is_type(dtype) || !is_type(table_dtype)) return fail(PB_E_INVALID, "types must be PB_F32 or PB_BF16");
+  if (add != 0 && add != 1) return fail(PB_E_INVALID, "add must be 0 or 1");
+  const int64_t need = pb_embed_backward_workspace(n, vocab, dim);
+  if (need < 0) return fail(PB_E_INVALID, "bad sizes: a table of %lld rows of %lld, %lld ids", (long long)vocab, (long long)dim, (long long)n);
+  if (const int rc = bad_ids("ids", ids, id_bits)) return rc;
+  if (n == 0 && add) return PB_OK;
+  if (!d_table || (n > 0 && (!d_out || !ids))) return fail(PB_E_INVALID, "NULL argument");
+  if (!aligned(d_out, size_of(dtype)) || !aligned(d_table, size_of(table_dtype))) return fail(PB_E_INVALID, "arrays must lie on boundaries of their element size");
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
+    return fail(PB_E_INVALID, "workspace: %lld bytes on a 16-byte boundary are needed", (long long)need);
+  launch_embed_grad({d_out, vocab, dim, n, ids, scale, d_table, add, workspace}, dtype, table_dtype, id_bits, (hipStream_t)stream);
+  return launched();
+}
+
+}  // extern "C"

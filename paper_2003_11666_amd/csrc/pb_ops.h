@@ -1,0 +1,101 @@
+// Operators over plain device arrays (pb_adamw.hip, pb_logprob.hip, pb_embed.hip; their C entries in pb_ops.cpp): what the
+// kernels and the checks in front of them share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/pb.h"
+
+namespace pb {
+
+int fail(int code, const char* fmt, ...);   // pb_host.cpp: the text of pb_last_error, returns code
+
+// ------------------------------------------------------------------------------------------------ AdamW (pb_adamw.hip)
+constexpr int ADAMW_TENSORS = 64;    // tensors per launch: a lane each in the search for a workgroup's tensor, 3 KB of arguments
+constexpr int ADAMW_CHUNK = PB_ADAMW_BLOCK;   // elements per workgroup
+
+struct AdamWArgs {
+  void* w[ADAMW_TENSORS];
+  const void* g[ADAMW_TENSORS];
+  void* hat[ADAMW_TENSORS];
+  int64_t n[ADAMW_TENSORS];
+  int64_t at[ADAMW_TENSORS];           // where the tensor's moments start
+  int32_t first[ADAMW_TENSORS];        // its first workgroup
+  float decay[ADAMW_TENSORS];          // lr * weight_decay
+  int32_t n_tensors;
+  float b1, c1, b2, c2, eps, horizon;  // c = 1 - b
+  double lr, beta1, beta2;
+  int64_t step;
+  const int64_t* step_dev;
+  const float* grad_scale;
+  uint64_t seed;
+  void *m, *v;
+  uint8_t *m_exp, *v_exp;
+};
+void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, int hat_type, int bits, hipStream_t s);
+void launch_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, hipStream_t s);
+
+// ------------------------------------------------------------------------------------ log probabilities (pb_logprob.hip)
+struct LogpArgs {
+  const void* logits;
+  int64_t rows, vocab, stride;
+  const void* targets;
+  float scale;
+  float *logp, *entropy, *norm;
+  int32_t top;
+  float* top_logp;
+  void* top_ids;
+  void* workspace;
+};
+int64_t logp_workspace(int64_t rows, int64_t vocab, int top);
+void launch_logp(const LogpArgs& a, int dtype, int id_bits, hipStream_t s);
+
+struct LogpGradArgs {
+  const void* logits;
+  int64_t rows, vocab, stride;
+  const void* targets;
+  float scale;
+  const float *norm, *entropy, *g_logp, *g_entropy;
+  void* d;
+  int64_t d_stride;
+};
+void launch_logp_grad(const LogpGradArgs& a, int dtype, int id_bits, hipStream_t s);
+
+// -------------------------------------------------------------------------------------------- embeddings (pb_embed.hip)
+struct EmbedArgs {
+  const void* table;
+  int64_t vocab, dim, n;
+  const void* ids;
+  float scale;
+  void* out;
+};
+void launch_embed(const EmbedArgs& a, int dtype, int out_dtype, int id_bits, hipStream_t s);
+
+struct EmbedGradArgs {
+  const void* d_out;
+  int64_t vocab, dim, n;
+  const void* ids;
+  float scale;
+  void* d_table;
+  int32_t add;
+  void* workspace;
+};
+int64_t embed_grad_workspace(int64_t n, int64_t vocab, int64_t dim);
+void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int id_bits, hipStream_t s);
+
+// ------------------------------------------------------------------------------------------------ what kernels share
+#ifdef __HIPCC__
+struct bf16 { uint16_t bits; };
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(bf16 x) { return __uint_as_float((uint32_t)x.bits << 16); }
+template <class T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float x) { return __builtin_bit_cast(bf16, (__bf16)x); }   // to nearest, ties to even
+
+// f(T{}, U{}) with the C++ types of two pb_dtype
+template <class F> void with_type(int t, F&& f) { t == PB_BF16 ? f(bf16()) : f(float()); }
+template <class F> void with_id(int bits, F&& f) { bits == 64 ? f(int64_t()) : f(int32_t()); }
+#endif
+
+}  // namespace pb

@@ -1,0 +1,284 @@
+"""Operators over plain device tensors: AdamW over many tensors at once, log probabilities of given tokens and their
+gradient, embedding lookup and its gradient (the functions of include/pb.h beside pb_update_standalone, which defines them).
+Argument marshalling and checks only; PyTorch provides the memory and the stream.  Nothing here is recorded by autograd."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple, Optional
+
+import numpy as np
+
+from .binding import PBError, _check, load_library
+
+ADAMW_BLOCK = 128
+_TENSOR = np.dtype([("w", "u8"), ("g", "u8"), ("w_hat", "u8"), ("n", "i8"), ("weight_decay", "f8")])
+_READY = None
+
+
+class _AdamWDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("w_type", "g_type", "w_hat_type", "moment_bits")] \
+        + [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "horizon")] \
+        + [("step", C.c_int64), ("step_dev", C.c_void_p), ("grad_scale", C.c_void_p), ("seed", C.c_uint64)]
+
+
+def _library():
+    global _READY
+    lib = load_library()
+    if _READY is lib:
+        return lib
+    p, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+    for name, result, args in (
+            ("pb_adamw_elements", i64, [p, i32]),
+            ("pb_adamw_step", C.c_int, [p, i32, p, p, p, p, p, p]),
+            ("pb_adamw_moments", C.c_int, [p, p, p, p, i64, p, p, p]),
+            ("pb_log_probs_workspace", i64, [i64, i64, i32]),
+            ("pb_log_probs", C.c_int, [p, i32, i64, i64, i64, p, i32, f32, p, p, p, i32, p, p, p, i64, p]),
+            ("pb_log_probs_backward", C.c_int, [p, i32, i64, i64, i64, p, i32, f32, p, p, p, p, p, i64, p]),
+            ("pb_embed", C.c_int, [p, i32, i64, i64, p, i32, i64, f32, p, i32, p]),
+            ("pb_embed_backward_workspace", i64, [i64, i64, i64]),
+            ("pb_embed_backward", C.c_int, [p, i32, p, i32, i64, i64, i64, f32, p, i32, i32, p, i64, p])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = result, args
+    _READY = lib
+    return lib
+
+
+def _type(t, what):
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise PBError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+
+
+def _bits(ids, what):
+    import torch
+    if ids.dtype == torch.int64:
+        return 64
+    if ids.dtype == torch.int32:
+        return 32
+    raise PBError(f"{what} must be int32 or int64, not {ids.dtype}")
+
+
+def _on_gpu(what, *tensors):
+    """The GPU that holds all of them (None among them is passed over)."""
+    index = {t.get_device() for t in tensors if t is not None}
+    if len(index) != 1 or -1 in index:
+        raise PBError(f"{what}: all tensors must be on one GPU")
+    return index.pop()
+
+
+def _dense(what, *tensors):
+    for t in tensors:
+        if t is not None and not t.is_contiguous():
+            raise PBError(f"{what}: tensors must be contiguous")
+
+
+def _floats(what, shape, *tensors):
+    import torch
+    for t in tensors:
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+            raise PBError(f"{what} must be contiguous float32 of shape {tuple(shape)}")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(index, f, *args):
+    """f(*args, stream) on the current stream of GPU `index`, with that GPU current."""
+    import torch
+    if torch.cuda.current_device() == index:
+        return _check(load_library(), f(*args, torch.cuda.current_stream().cuda_stream))
+    with torch.cuda.device(index):
+        return _check(load_library(), f(*args, torch.cuda.current_stream().cuda_stream))
+
+
+# ----------------------------------------------------------------------------------------------------------------- AdamW
+def adamw_elements(params):
+    """Entries of the flat moment tensors of adamw_step for these parameters; 8-bit moments have a block exponent for
+    every ADAMW_BLOCK of them.  Zeros are the moments that training starts with."""
+    lib = _library()
+    n = np.array([p.numel() for p in params], dtype=np.int64)
+    return _check(lib, lib.pb_adamw_elements(n.ctypes.data, len(n)))
+
+
+def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, m_exp=None, v_exp=None, seed=0,
+               grad_scale=None, predicted=None, horizon=0.0):
+    """One AdamW step over all tensors of `params` in place, and its moments m, v (pb_adamw_step).
+
+    params, grads: lists of contiguous tensors of the same sizes, each list float32 or bfloat16.  m, v: flat tensors of
+    adamw_elements(params) entries, float32, or uint8 with block exponents m_exp, v_exp (uint8, an ADAMW_BLOCK-th as many).
+    step: counted from 1, or an int64 tensor of one element on the GPU.  weight_decay: a number, or one for each tensor.
+    grad_scale: None or a float32 tensor of one element on the GPU that gradients are multiplied by.  predicted: None, or
+    tensors that receive the weights as they will be after `horizon` more such steps (0: copies, in their own type)."""
+    import torch
+    lib = _library()
+    params, grads = list(params), list(grads)
+    n = len(params)
+    hats = [] if predicted is None else list(predicted)
+    if len(grads) != n or (predicted is not None and len(hats) != n):
+        raise PBError("adamw_step: one gradient (and predicted tensor) for each parameter")
+    d = _AdamWDesc()
+    step_dev = step if isinstance(step, torch.Tensor) else None
+    for t, kind, what in ((step_dev, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale")):
+        if t is not None and (t.dtype != kind or t.numel() != 1):
+            raise PBError(f"adamw_step: {what} must be one element of {kind}")
+    index = _on_gpu("adamw_step", m, v, m_exp, v_exp, step_dev, grad_scale, *params, *grads, *hats)
+    _dense("adamw_step", m, v, m_exp, v_exp, *params, *grads, *hats)
+    sizes = [p.numel() for p in params]
+    for ts in (grads, hats):
+        if ts and [t.numel() for t in ts] != sizes:
+            raise PBError("adamw_step: gradients and predicted tensors must have their parameters' sizes")
+    for name, ts in (("w_type", params), ("g_type", grads), ("w_hat_type", hats)):
+        if len({t.dtype for t in ts}) > 1:
+            raise PBError("adamw_step: the tensors of a list must be of one type")
+        if ts:
+            setattr(d, name, _type(ts[0], "adamw_step: tensors"))
+    rec = np.zeros(n, dtype=_TENSOR)
+    rec["w"] = [p.data_ptr() for p in params]
+    rec["g"] = [g.data_ptr() for g in grads]
+    if hats:
+        rec["w_hat"] = [h.data_ptr() for h in hats]
+    rec["n"] = sizes
+    rec["weight_decay"] = weight_decay
+    total = int((-(-rec["n"] // ADAMW_BLOCK) * ADAMW_BLOCK).sum())
+    eight = m.dtype == torch.uint8
+    if v.dtype != m.dtype or m.dtype not in (torch.uint8, torch.float32) or m.numel() != total or v.numel() != total:
+        raise PBError(f"adamw_step: m and v must be flat float32 or uint8 of {total} elements")
+    for t in (m_exp, v_exp):
+        if eight != (t is not None) or (eight and (t.dtype != torch.uint8 or t.numel() != total // ADAMW_BLOCK)):
+            raise PBError(f"adamw_step: 8-bit moments, and only they, have exponents: uint8 of {total // ADAMW_BLOCK} elements")
+    d.moment_bits = 8 if eight else 32
+    d.lr, (d.beta1, d.beta2), d.eps, d.horizon = lr, betas, eps, horizon
+    d.step = 0 if step_dev is not None else int(step)
+    d.step_dev, d.grad_scale, d.seed = _ptr(step_dev), _ptr(grad_scale), int(seed) & 0xFFFFFFFFFFFFFFFF
+    _call(index, lib.pb_adamw_step, rec.ctypes.data, n, C.byref(d), m.data_ptr(), v.data_ptr(), _ptr(m_exp), _ptr(v_exp))
+
+
+def adamw_moments(m, v, m_exp, v_exp):
+    """What 8-bit moments stand for: two float32 tensors (pb_adamw_moments)."""
+    import torch
+    lib = _library()
+    for t in (m, v, m_exp, v_exp):
+        if t.dtype != torch.uint8:
+            raise PBError("adamw_moments: codes and exponents must be uint8")
+    if v.numel() != m.numel() or m_exp.numel() * ADAMW_BLOCK != m.numel() or v_exp.numel() != m_exp.numel():
+        raise PBError(f"adamw_moments: one exponent for every {ADAMW_BLOCK} codes")
+    index = _on_gpu("adamw_moments", m, v, m_exp, v_exp)
+    _dense("adamw_moments", m, v, m_exp, v_exp)
+    out = torch.empty(2, m.numel(), dtype=torch.float32, device=m.device)
+    _call(index, lib.pb_adamw_moments, m.data_ptr(), v.data_ptr(), m_exp.data_ptr(), v_exp.data_ptr(), m.numel(), out[0].data_ptr(), out[1].data_ptr())
+    return out[0], out[1]
+
+
+# ----------------------------------------------------------------------------------------------------- log probabilities
+class LogProbs(NamedTuple):
+    logp: Optional["torch.Tensor"]       # noqa: F821
+    entropy: Optional["torch.Tensor"]    # noqa: F821
+    norm: "torch.Tensor"                 # noqa: F821  what log_probs_backward takes: maximum and ln of the sum of each row
+    top_logp: Optional["torch.Tensor"]   # noqa: F821
+    top_ids: Optional["torch.Tensor"]    # noqa: F821
+
+
+def _rows(logits, what):
+    """(rows, vocab, row stride) of logits [..., vocab] with neighbouring logits side by side."""
+    if logits.dim() == 2:
+        rows, vocab = logits.shape
+        if vocab > 1 and logits.stride(1) != 1:
+            raise PBError(f"{what}: the logits of a row must lie side by side")
+        return rows, vocab, logits.stride(0) if rows > 1 else vocab
+    if logits.dim() == 0 or not logits.is_contiguous():
+        raise PBError(f"{what}: logits must be [rows, vocab], or contiguous with any number of leading dimensions")
+    vocab = logits.shape[-1]
+    return (logits.numel() // vocab if vocab else 0), vocab, vocab
+
+
+def _targets(targets, shape, what):
+    if targets is None:
+        return 64
+    if tuple(targets.shape) != tuple(shape) or not targets.is_contiguous():
+        raise PBError(f"{what}: targets must be contiguous, one for each row: shape {tuple(shape)}")
+    return _bits(targets, f"{what}: targets")
+
+
+def log_probs(logits, targets=None, *, scale=1.0, top=0, entropy=True):
+    """Log probability of targets under softmax(scale * logits), entropy and the `top` best alternatives of each row
+    (pb_log_probs).  logits: [..., vocab], float32 or bfloat16; targets: int32 or int64 of the leading shape, or None."""
+    import torch
+    lib = _library()
+    kind = _type(logits, "log_probs: logits")
+    index = _on_gpu("log_probs", logits, targets)
+    rows, vocab, stride = _rows(logits, "log_probs")
+    lead = logits.shape[:-1]
+    bits = _targets(targets, lead, "log_probs")
+    top = int(top)
+    need = _check(lib, lib.pb_log_probs_workspace(rows, vocab, top))
+    new = lambda shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+    r = LogProbs(new(lead) if targets is not None else None, new(lead) if entropy else None, new((*lead, 2)),
+                 new((*lead, top)) if top else None, new((*lead, top), torch.int64 if bits == 64 else torch.int32) if top else None)
+    ws = new(need, torch.uint8) if need else None
+    _call(index, lib.pb_log_probs, logits.data_ptr(), kind, rows, vocab, stride, _ptr(targets), bits, scale, _ptr(r.logp), _ptr(r.entropy),
+          r.norm.data_ptr(), top, _ptr(r.top_logp), _ptr(r.top_ids), _ptr(ws), need)
+    return r
+
+
+def log_probs_backward(logits, targets, norm, g_logp, *, entropy=None, g_entropy=None, scale=1.0, out=None):
+    """Gradient with respect to the logits of sum(g_logp * logp) + sum(g_entropy * entropy) (pb_log_probs_backward).
+    norm, entropy: of log_probs for the same logits and scale.  g_logp, g_entropy: float32 of the rows' shape, or None.
+    out: None, or a tensor like the logits (it may be the logits themselves)."""
+    import torch
+    lib = _library()
+    kind = _type(logits, "log_probs_backward: logits")
+    rows, vocab, stride = _rows(logits, "log_probs_backward")
+    lead = logits.shape[:-1]
+    bits = _targets(targets, lead, "log_probs_backward")
+    _floats("log_probs_backward: norm", (*lead, 2), norm)
+    _floats("log_probs_backward: entropy, g_logp and g_entropy", lead, entropy, g_logp, g_entropy)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if out.dtype != logits.dtype or out.shape != logits.shape:
+        raise PBError("log_probs_backward: out must have the logits' shape and type")
+    index = _on_gpu("log_probs_backward", logits, targets, norm, g_logp, entropy, g_entropy, out)
+    d_stride = _rows(out, "log_probs_backward")[2]
+    _call(index, lib.pb_log_probs_backward, logits.data_ptr(), kind, rows, vocab, stride, _ptr(targets), bits, scale, norm.data_ptr(), _ptr(entropy),
+          _ptr(g_logp), _ptr(g_entropy), out.data_ptr(), d_stride)
+    return out
+
+
+# ------------------------------------------------------------------------------------------------------------ embeddings
+def _table(table, what):
+    if table.dim() != 2 or not table.is_contiguous():
+        raise PBError(f"{what}: the table must be contiguous [vocab, dim]")
+    return table.shape
+
+
+def embed(table, ids, *, scale=1.0, dtype=None):
+    """scale * table[ids] in `dtype` (the table's by default), zeros for ids outside the table (pb_embed)."""
+    import torch
+    lib = _library()
+    kind, bits = _type(table, "embed: table"), _bits(ids, "embed: ids")
+    vocab, dim = _table(table, "embed")
+    _dense("embed", ids)
+    index = _on_gpu("embed", table, ids)
+    out = torch.empty((*ids.shape, dim), dtype=dtype or table.dtype, device=table.device)
+    _call(index, lib.pb_embed, table.data_ptr(), kind, vocab, dim, ids.data_ptr(), bits, ids.numel(), scale, out.data_ptr(), _type(out, "embed: out"))
+    return out
+
+
+def embed_backward(d_out, ids, d_table, *, scale=1.0, add=False):
+    """Gradient of the table of embed(): written into d_table [vocab, dim], or added to it (pb_embed_backward)."""
+    import torch
+    lib = _library()
+    kind, bits = _type(d_out, "embed_backward: d_out"), _bits(ids, "embed_backward: ids")
+    vocab, dim = _table(d_table, "embed_backward")
+    if tuple(d_out.shape) != (*ids.shape, dim):
+        raise PBError(f"embed_backward: d_out must be of shape {(*ids.shape, dim)}")
+    _dense("embed_backward", d_out, ids)
+    index = _on_gpu("embed_backward", d_out, ids, d_table)
+    need = _check(lib, lib.pb_embed_backward_workspace(ids.numel(), vocab, dim))
+    ws = torch.empty(need, dtype=torch.uint8, device=d_table.device) if need else None
+    _call(index, lib.pb_embed_backward, d_out.data_ptr(), kind, ids.data_ptr(), bits, ids.numel(), vocab, dim, scale, d_table.data_ptr(),
+          _type(d_table, "embed_backward: d_table"), int(bool(add)), _ptr(ws), need)
+    return d_table

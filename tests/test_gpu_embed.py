@@ -1,0 +1,174 @@
+"""embed and embed_backward against their definitions: a lookup is one product and one rounding, a gradient's sums lie within
+the bounds of their roundings."""
+import numpy as np
+import pytest
+
+from tests import operator_refs as R
+
+pytestmark = pytest.mark.gpu
+TYPES = ["float32", "bfloat16"]
+
+
+def table(rows, dim, dtype, seed=0):
+    import torch
+    return (torch.randn(rows, dim, generator=torch.Generator().manual_seed(seed)) * 0.5).to(getattr(torch, dtype)).cuda()
+
+
+def tokens(n, vocab, kind="uniform", bits=64, seed=1):
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    u = torch.rand(n, generator=gen, dtype=torch.float64)
+    ids = {"uniform": (u * vocab).long(), "skewed": (u ** 6 * vocab).long(), "one": torch.full((n,), vocab // 2), "none": torch.full((n,), -1),
+           "rising": torch.arange(n) % vocab, "falling": vocab - 1 - torch.arange(n) % vocab}[kind].clamp(max=vocab - 1)
+    if kind not in ("one", "none"):
+        ids[2::7] = -1
+        ids[4::13] = vocab
+    return ids.to(torch.int64 if bits == 64 else torch.int32).cuda()
+
+
+@pytest.mark.parametrize("n,dim,vocab", [(1, 1, 1), (1, 4096, 500), (3, 5, 7), (64, 4096, 100), (1000, 33, 50), (129, 128, 300), (70000, 8, 10), (5, 12345, 9)])
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("out", TYPES)
+def test_lookup(n, dim, vocab, kind, out):
+    import torch
+    from paper_2003_11666_amd import embed
+    w, ids, scale = table(vocab, dim, kind), tokens(n, vocab, bits=32 if n % 2 else 64), 0.3
+    got = embed(w, ids, scale=scale, dtype=getattr(torch, out))
+    i = ids.long()
+    there = (i >= 0) & (i < vocab)
+    ref = torch.where(there[:, None], w[i.clamp(0, vocab - 1)].float() * torch.tensor(scale, device="cuda"), 0.0).to(got.dtype)
+    assert torch.equal(got, ref)
+
+
+def test_lookup_of_shapes_and_special_values():
+    import torch
+    from paper_2003_11666_amd import embed
+    w = table(10, 6, "float32")
+    w[3, 2], w[4] = float("nan"), float("inf")
+    ids = torch.tensor([[3, -1, 4], [2 ** 40, -2 ** 40, 9]], device="cuda")
+    got = embed(w, ids)
+    assert got.shape == (2, 3, 6) and torch.isnan(got[0, 0, 2]) and torch.isinf(got[0, 2]).all()
+    assert torch.all(got[0, 1] == 0) and torch.all(got[1, :2] == 0) and torch.equal(got[1, 2], w[9])
+    assert embed(w, ids[:0]).shape == (0, 3, 6)
+    assert torch.equal(embed(w, ids[1, 2]), w[9])
+
+
+def check_grad(g, ids, start, *, scale=0.7, add=True, call=None):
+    import torch
+    from paper_2003_11666_amd import embed_backward
+    d = start.clone()
+    got = (call or (lambda f: f()))(lambda: embed_backward(g, ids, d, scale=scale, add=add))
+    torch.cuda.synchronize()
+    assert got is d
+    ref, bound = R.embed_grad(R.f64(g), ids.cpu().numpy(), R.f64(start), start.shape[0], float(np.float32(scale)), add, R.HALF[str(start.dtype).split(".")[1]])
+    err = np.abs(R.f64(d) - ref)
+    assert np.all(err <= bound), np.max(err - bound)
+    return d
+
+
+@pytest.mark.parametrize("add", [True, False])
+@pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "none", "rising", "falling"])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 1000, 4097, 20000, 70001])
+def test_gradient(n, kind, add):
+    g = table(n, 24, "float32", seed=n)
+    for vocab in (1, 2, 300, 70000):
+        check_grad(g, tokens(n, vocab, kind, bits=32), table(vocab, 24, "float32", seed=5), add=add)
+
+
+@pytest.mark.parametrize("dim", [1, 3, 8, 64, 65, 255, 1000, 1024, 4100])
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("add", [True, False])
+def test_gradient_widths_and_types(dim, kind, out, add):
+    check_grad(table(500, dim, kind, seed=2), tokens(500, 90, "skewed"), table(90, dim, out, seed=3), add=add)
+
+
+def test_gradient_of_arrays_off_16_byte_boundaries():
+    import torch
+    n, dim, vocab = 300, 33, 40
+    g = torch.randn(n * dim + 3, device="cuda")[3:].view(n, dim)
+    d = torch.randn(vocab * dim + 1, device="cuda").bfloat16()[1:].view(vocab, dim)
+    ids = tokens(n + 1, vocab)[1:]
+    from paper_2003_11666_amd import embed, embed_backward
+    start = R.f64(d)
+    embed_backward(g, ids, d, add=True)
+    ref, bound = R.embed_grad(R.f64(g), ids.cpu().numpy(), start, vocab, 1.0, True, R.HALF["bfloat16"])
+    assert np.all(np.abs(R.f64(d) - ref) <= bound)
+    w = torch.randn(vocab * dim + 1, device="cuda")[1:].view(vocab, dim)
+    there = (ids >= 0) & (ids < vocab)
+    assert torch.equal(embed(w, ids), torch.where(there[:, None], w[ids.clamp(0, vocab - 1)], 0.0))
+
+
+def test_gradient_of_no_tokens():
+    import torch
+    from paper_2003_11666_amd import embed_backward
+    d = table(9, 5, "float32")
+    before = d.clone()
+    g, ids = torch.empty(0, 5, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    assert torch.equal(embed_backward(g, ids, d, add=True), before)
+    assert torch.all(embed_backward(g, ids, d) == 0)
+
+
+def test_rows_without_a_token_are_left_alone():
+    """Also what a sum with zero would change: a NaN stays, minus zero stays."""
+    import torch
+    from paper_2003_11666_amd import embed_backward
+    d = torch.full((6, 40), -0.0, device="cuda")
+    d[2] = float("nan")
+    ids = torch.tensor([4, -1, 4, 99], device="cuda")
+    g = torch.ones(4, 40, device="cuda")
+    g[1] = g[3] = float("nan")                       # padding's gradients count for nothing, whatever they hold
+    embed_backward(g, ids, d, add=True)
+    assert torch.isnan(d[2]).all() and torch.all(d[4] == 2)
+    rest = d[[0, 1, 3, 5]]
+    assert torch.all(rest == 0) and torch.all(torch.signbit(rest))
+
+
+def test_same_bits_again_on_another_stream_and_replayed():
+    import torch
+    from paper_2003_11666_amd import embed, embed_backward
+    n, dim, vocab = 30000, 136, 5000
+    g, ids, start = table(n, dim, "bfloat16"), tokens(n, vocab, "skewed"), table(vocab, dim, "float32", seed=8)
+    first = check_grad(g, ids, start)
+    side = torch.cuda.Stream()
+
+    def on_side(f):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            r = f()
+        torch.cuda.current_stream().wait_stream(side)
+        return r
+
+    assert torch.equal(check_grad(g, ids, start, call=on_side), first)
+    d = start.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        e = embed(start, ids, scale=2.0)
+        embed_backward(g, ids, d, scale=0.7, add=True)
+    eager = start.clone()
+    for k in range(4):
+        ids.copy_(tokens(n, vocab, ["skewed", "uniform", "one", "rising"][k], seed=k))
+        graph.replay()
+        embed_backward(g, ids, eager, scale=0.7, add=True)
+        torch.cuda.synchronize()
+        assert torch.equal(d, eager) and torch.equal(e, embed(start, ids, scale=2.0)), k
+
+
+def test_tables_beyond_32_bit_offsets():
+    """A table of 2^32 + elements: its last rows are looked up, and receive gradients."""
+    import torch
+    from paper_2003_11666_amd import embed, embed_backward
+    vocab, dim = (1 << 20) + 3, 4096
+    w = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([vocab - 1, vocab - 2, 0, vocab, vocab - 1], device="cuda")
+    w[ids[:3]] = table(3, dim, "bfloat16")
+    got = embed(w, ids)
+    assert torch.equal(got[:3], w[ids[:3]]) and torch.all(got[3] == 0) and torch.equal(got[4], got[0])
+    before = w[ids[:3]].double()
+    g = table(5, dim, "bfloat16", seed=4)
+    embed_backward(g, ids, w, add=True)
+    ref = before + torch.stack([g[0].double() + g[4].double(), g[1].double(), g[2].double()])
+    # one rounding to bf16 of the result, and one 32-bit one in each of two sums
+    bound = 2.0 ** -8 * ref.abs() + 4 * 2.0 ** -24 * (before.abs() + 2 * g.double().abs().max())
+    assert torch.all((w[ids[:3]].double() - ref).abs() <= bound)
