@@ -35,13 +35,14 @@ __device__ __forceinline__ uint32_t encode_v(float x, uint32_t dither, int e) {
   return bits == 0 ? 0u : c < 1 ? 1u : c > 255 ? 255u : (uint32_t)c;
 }
 
-struct Coeffs { float lr, rs; };   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+struct Coeffs { float lr, root; };   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
 __device__ __forceinline__ double power(double x, int64_t t) {
   double r = 1.0;
   for (; t > 0; t >>= 1, x *= x)
     if (t & 1) r *= x;
   return r;
 }
+// ... of the step whose number lies in device memory
 __device__ __forceinline__ Coeffs coeffs(const AdamWArgs& a, int64_t t) {
   if (t < 1) return {__uint_as_float(0x7FC00000u), 0.f};
   return {(float)(a.lr / (1.0 - power(a.beta1, t))), (float)(1.0 / sqrt(1.0 - power(a.beta2, t)))};
@@ -54,81 +55,164 @@ __device__ __forceinline__ int tensor_of(const AdamWArgs& a, int group) {
   return __builtin_amdgcn_readfirstlane((int)__popcll(__ballot(before)) - 1);
 }
 
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, CTRL, 0xF, 0xF, false));
+}
+// Largest over each row of 16 lanes: the lanes that share a block of 128 elements, 8 each.
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+  return dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(x))));
+}
+static_assert(PB_ADAMW_BLOCK == 128, "16 lanes of 8 elements");
+
+constexpr int AT = 256;   // threads per workgroup
+
+// Bound by memory: 24 bytes an element with 32-bit moments, weights and gradients.  A thread takes vectors of V elements, 16
+// bytes of the 32-bit arrays or of bf16 with 8-bit moments, and requests all of its U vectors before it uses the first; the
+// arrays are passed over once per step, so every access carries the non-temporal hint.
 template <class W, class G, class H, int BITS>
-__global__ void __launch_bounds__(ADAMW_CHUNK) k_adamw(const AdamWArgs a) {
-  __shared__ uint32_t top[2][ADAMW_CHUNK];
-  const int t = tensor_of(a, (int)blockIdx.x), tid = threadIdx.x;
-  const int64_t i = (int64_t)((int)blockIdx.x - a.first[t]) * ADAMW_CHUNK + tid, at = a.at[t] + i;
-  const int64_t step = a.step_dev ? *a.step_dev : a.step;
-  const Coeffs k = coeffs(a, step);
-  const bool mine = i < a.n[t];
-  float m = 0.f, v = 0.f, g = 0.f, w = 0.f;
-  if (mine) {
-    g = to_float(((const G*)a.g[t])[i]);
-    w = to_float(((const W*)a.w[t])[i]);
-    if (a.grad_scale) g *= *a.grad_scale;
-    if (BITS == 32) {
-      m = ((const float*)a.m)[at];
-      v = ((const float*)a.v)[at];
+__global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
+  constexpr int V = BITS == 8 ? 8 : 4, U = ADAMW_CHUNK / (AT * V);
+  const int t = tensor_of(a, (int)blockIdx.x);
+  const int64_t n = a.n[t], i0 = (int64_t)((int)blockIdx.x - a.first[t]) * ADAMW_CHUNK + threadIdx.x * V;
+  const bool vec = a.vec[t];
+  W* w = (W*)a.w[t];
+  const G* g = (const G*)a.g[t];
+  H* hat = (H*)a.hat[t];
+  const int64_t at0 = a.at[t] + i0;
+  float wv[U][V], gv[U][V], mv[U][V], vv[U][V];
+  uint32_t mc[U][2], vc[U][2];
+  int em[U], ev[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
+    if ((i & ~(int64_t)(PB_ADAMW_BLOCK - 1)) >= n) continue;   // (whole blocks: their lanes take the maximum together)
+    if (vec && i + V <= n) {
+      load_pack<W, V>(wv[u], w + i);
+      load_pack<G, V>(gv[u], g + i);
     } else {
-      m = decode_m(((const uint8_t*)a.m)[at], a.m_exp[at / PB_ADAMW_BLOCK]);
-      v = decode_v(((const uint8_t*)a.v)[at], a.v_exp[at / PB_ADAMW_BLOCK]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        wv[u][e] = i + e < n ? to_float(w[i + e]) : 0.f;
+        gv[u][e] = i + e < n ? to_float(g[i + e]) : 0.f;
+      }
     }
-    // (each operation rounded: which code an 8-bit moment gets is defined by that)
-    m = a.b1 * m + a.c1 * g;
-    v = a.b2 * v + a.c2 * (g * g);
-    const float d = k.lr * (m / (sqrtf(v) * k.rs + a.eps));
-    w = w - a.decay[t] * w - d;
-    ((W*)a.w[t])[i] = from_float<W>(w);
-    if (a.hat[t]) ((H*)a.hat[t])[i] = from_float<H>(w - a.horizon * d);
-  }
-  if (BITS == 32) {
-    if (mine) {
-      ((float*)a.m)[at] = m;
-      ((float*)a.v)[at] = v;
+    if constexpr (BITS == 32) {   // (entries up to the next multiple of a block belong to the tensor)
+      load_pack<float, V>(mv[u], (const float*)a.m + at);
+      load_pack<float, V>(vv[u], (const float*)a.v + at);
+    } else {
+      typedef uint32_t two __attribute__((ext_vector_type(2)));
+      const two m2 = __builtin_nontemporal_load((const two*)((const uint8_t*)a.m + at)), v2 = __builtin_nontemporal_load((const two*)((const uint8_t*)a.v + at));
+      mc[u][0] = m2.x; mc[u][1] = m2.y; vc[u][0] = v2.x; vc[u][1] = v2.y;
+      em[u] = a.m_exp[at / PB_ADAMW_BLOCK];
+      ev[u] = a.v_exp[at / PB_ADAMW_BLOCK];
     }
-    return;
   }
-  top[0][tid] = __float_as_uint(m) & 0x7FFFFFFF;
-  top[1][tid] = __float_as_uint(v) & 0x7FFFFFFF;
-  __syncthreads();
-  for (int s = ADAMW_CHUNK / 2; s > 0; s >>= 1) {
-    if (tid < s) {
-      top[0][tid] = max(top[0][tid], top[0][tid + s]);
-      top[1][tid] = max(top[1][tid], top[1][tid + s]);
+  const int64_t step = a.step_dev ? *a.step_dev : a.step;
+  const Coeffs k = a.step_dev ? coeffs(a, step) : Coeffs{a.lr_t, a.root_t};
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f, decay = a.decay[t];
+  const uint64_t key = BITS == 8 ? mix(a.seed ^ mix((uint64_t)step)) : 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
+    if ((i & ~(int64_t)(PB_ADAMW_BLOCK - 1)) >= n) continue;
+    float hv[V];
+    uint32_t tm = 0, tv = 0;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const bool mine = i + e < n;
+      float m = mv[u][e], v = vv[u][e];
+      if constexpr (BITS == 8) {
+        m = decode_m(mc[u][e / 4] >> 8 * (e % 4) & 255, em[u]);
+        v = decode_v(vc[u][e / 4] >> 8 * (e % 4) & 255, ev[u]);
+      }
+      const float grad = gv[u][e] * gs;
+      // (each operation rounded: which code an 8-bit moment gets is defined by that)
+      m = a.b1 * m + a.c1 * grad;
+      v = a.b2 * v + a.c2 * (grad * grad);
+      const float d = k.lr * (m / fmaf(sqrtf(v), k.root, a.eps));
+      const float w2 = fmaf(-decay, wv[u][e], wv[u][e]) - d;
+      wv[u][e] = w2;
+      hv[e] = fmaf(-a.horizon, d, w2);
+      mv[u][e] = mine ? m : 0.f;
+      vv[u][e] = mine ? v : 0.f;
+      if (BITS == 8) {
+        tm = max(tm, __float_as_uint(mv[u][e]) & 0x7FFFFFFF);
+        tv = max(tv, __float_as_uint(vv[u][e]) & 0x7FFFFFFF);
+      }
     }
-    __syncthreads();
-  }
-  const int em = block_exponent(top[0][0]), ev = block_exponent(top[1][0]);
-  const uint64_t key = mix(a.seed ^ mix((uint64_t)step));
-  const uint64_t z = mix((uint64_t)(at >> 1) * GOLDEN + key) >> (at & 1 ? 32 : 0);
-  ((uint8_t*)a.m)[at] = encode_m(m, (uint32_t)(z & 0xFFFF) << 4 | 8, em);
-  ((uint8_t*)a.v)[at] = encode_v(v, (uint32_t)(z >> 16 & 0xFFFF) << 4 | 8, ev);
-  if (tid == 0) {
-    a.m_exp[at / PB_ADAMW_BLOCK] = (uint8_t)em;
-    a.v_exp[at / PB_ADAMW_BLOCK] = (uint8_t)ev;
+    if (vec && i + V <= n) {
+      store_pack<W, V>(w + i, wv[u]);
+      if (hat) store_pack<H, V>(hat + i, hv);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if (i + e >= n) continue;
+        w[i + e] = from_float<W>(wv[u][e]);
+        if (hat) hat[i + e] = from_float<H>(hv[e]);
+      }
+    }
+    if constexpr (BITS == 32) {
+      if (i + V <= n) {
+        store_pack<float, V>((float*)a.m + at, mv[u]);
+        store_pack<float, V>((float*)a.v + at, vv[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (i + e >= n) continue;
+          ((float*)a.m)[at + e] = mv[u][e];
+          ((float*)a.v)[at + e] = vv[u][e];
+        }
+      }
+    } else {
+      const int m_top = block_exponent(row_max(tm)), v_top = block_exponent(row_max(tv));
+      uint32_t m2[2] = {0, 0}, v2[2] = {0, 0};
+#pragma unroll
+      for (int e = 0; e < V; ++e) {   // (one draw of 64 bits for two elements)
+        const uint32_t z = (uint32_t)(mix((uint64_t)((at >> 1) + e / 2) * GOLDEN + key) >> 32 * (e & 1));
+        m2[e / 4] |= encode_m(mv[u][e], (z & 0xFFFF) << 4 | 8, m_top) << 8 * (e % 4);
+        v2[e / 4] |= encode_v(vv[u][e], (z >> 16) << 4 | 8, v_top) << 8 * (e % 4);
+      }
+      typedef uint32_t two __attribute__((ext_vector_type(2)));
+      __builtin_nontemporal_store((two){m2[0], m2[1]}, (two*)((uint8_t*)a.m + at));
+      __builtin_nontemporal_store((two){v2[0], v2[1]}, (two*)((uint8_t*)a.v + at));
+      if ((threadIdx.x & 15) == 0) {
+        a.m_exp[at / PB_ADAMW_BLOCK] = (uint8_t)m_top;
+        a.v_exp[at / PB_ADAMW_BLOCK] = (uint8_t)v_top;
+      }
+    }
   }
 }
 
-__global__ void __launch_bounds__(256)
+int adamw_vector(int bits) { return bits == 8 ? 8 : 4; }
+
+// 8 codes of each moment per thread: 10 bytes an element, bound by memory.
+__global__ void __launch_bounds__(AT)
 k_adamw_moments(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v, const uint8_t* __restrict__ m_exp, const uint8_t* __restrict__ v_exp,
                 int64_t n, float* __restrict__ m_out, float* __restrict__ v_out) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    m_out[i] = decode_m(m[i], m_exp[i / PB_ADAMW_BLOCK]);
-    v_out[i] = decode_v(v[i], v_exp[i / PB_ADAMW_BLOCK]);
+  typedef uint32_t two __attribute__((ext_vector_type(2)));
+  const int64_t i = ((int64_t)blockIdx.x * AT + threadIdx.x) * 8;
+  if (i >= n) return;
+  const two mc = __builtin_nontemporal_load((const two*)(m + i)), vc = __builtin_nontemporal_load((const two*)(v + i));
+  const int em = m_exp[i / PB_ADAMW_BLOCK], ev = v_exp[i / PB_ADAMW_BLOCK];
+  float a[8], b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    a[e] = decode_m(mc[e / 4] >> 8 * (e % 4) & 255, em);
+    b[e] = decode_v(vc[e / 4] >> 8 * (e % 4) & 255, ev);
   }
+  store_pack<float, 8>(m_out + i, a);
+  store_pack<float, 8>(v_out + i, b);
 }
 
 void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, int hat_type, int bits, hipStream_t s) {
   with_type(w_type, [&](auto w) { with_type(g_type, [&](auto g) { with_type(hat_type, [&](auto h) {
-    if (bits == 32) hipLaunchKernelGGL((k_adamw<decltype(w), decltype(g), decltype(h), 32>), dim3((unsigned)groups), dim3(ADAMW_CHUNK), 0, s, a);
-    else hipLaunchKernelGGL((k_adamw<decltype(w), decltype(g), decltype(h), 8>), dim3((unsigned)groups), dim3(ADAMW_CHUNK), 0, s, a);
+    if (bits == 32) hipLaunchKernelGGL((k_adamw<decltype(w), decltype(g), decltype(h), 32>), dim3((unsigned)groups), dim3(AT), 0, s, a);
+    else hipLaunchKernelGGL((k_adamw<decltype(w), decltype(g), decltype(h), 8>), dim3((unsigned)groups), dim3(AT), 0, s, a);
   }); }); });
 }
 
 void launch_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, hipStream_t s) {
-  const int64_t want = (n + 255) / 256;
-  hipLaunchKernelGGL(k_adamw_moments, dim3((unsigned)(want < 8192 ? want : 8192)), dim3(256), 0, s, m, v, m_exp, v_exp, n, m_out, v_out);
+  hipLaunchKernelGGL(k_adamw_moments, dim3((unsigned)((n + 8 * AT - 1) / (8 * AT))), dim3(AT), 0, s, m, v, m_exp, v_exp, n, m_out, v_out);
 }
 
 }  // namespace pb

@@ -74,6 +74,10 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   a.eps = (float)d->eps; a.horizon = (float)d->horizon;
   a.lr = d->lr; a.beta1 = d->beta1; a.beta2 = d->beta2;
   a.step = d->step; a.step_dev = d->step_dev; a.grad_scale = d->grad_scale; a.seed = d->seed;
+  if (!d->step_dev) {
+    a.lr_t = (float)(d->lr / (1.0 - pow(d->beta1, (double)d->step)));
+    a.root_t = (float)(1.0 / sqrt(1.0 - pow(d->beta2, (double)d->step)));
+  }
   a.m = m; a.v = v; a.m_exp = m_exp; a.v_exp = v_exp;
   int64_t at = 0, groups = 0;
   auto launch = [&] {
@@ -94,6 +98,9 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
     const int k = a.n_tensors++;
     a.w[k] = t.w; a.g[k] = t.g; a.hat[k] = t.w_hat; a.n[k] = t.n; a.at[k] = at;
     a.first[k] = (int32_t)groups;
+    const size_t v = adamw_vector(d->moment_bits);
+    auto on = [&](const void* p, int type) { const size_t to = v * size_of(type); return aligned(p, to < 16 ? to : 16); };
+    a.vec[k] = on(t.w, d->w_type) && on(t.g, d->g_type) && on(t.w_hat, d->w_hat_type);
     a.decay[k] = (float)(d->lr * t.weight_decay);
     at += in_blocks(t.n) * PB_ADAMW_BLOCK;
     groups += g;
@@ -102,7 +109,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
 }
 
 int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, void* stream) {
-  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
+  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST / 2) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
   if (n == 0) return PB_OK;
   if (!m || !v || !m_exp || !v_exp || !m_out || !v_out) return fail(PB_E_INVALID, "NULL argument");
   if (((uintptr_t)m | (uintptr_t)v | (uintptr_t)m_out | (uintptr_t)v_out) % 16) return fail(PB_E_INVALID, "arrays must be 16-byte aligned");

@@ -13,7 +13,7 @@ int fail(int code, const char* fmt, ...);   // pb_host.cpp: the text of pb_last_
 
 // ------------------------------------------------------------------------------------------------ AdamW (pb_adamw.hip)
 constexpr int ADAMW_TENSORS = 64;    // tensors per launch: a lane each in the search for a workgroup's tensor, 3 KB of arguments
-constexpr int ADAMW_CHUNK = PB_ADAMW_BLOCK;   // elements per workgroup
+constexpr int ADAMW_CHUNK = 4096;    // elements per workgroup
 
 struct AdamWArgs {
   void* w[ADAMW_TENSORS];
@@ -24,7 +24,9 @@ struct AdamWArgs {
   int32_t first[ADAMW_TENSORS];        // its first workgroup
   float decay[ADAMW_TENSORS];          // lr * weight_decay
   int32_t n_tensors;
+  uint8_t vec[ADAMW_TENSORS];          // 1: its arrays lie on boundaries of a thread's vectors
   float b1, c1, b2, c2, eps, horizon;  // c = 1 - b
+  float lr_t, root_t;                  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t): of the step on the host
   double lr, beta1, beta2;
   int64_t step;
   const int64_t* step_dev;
@@ -33,6 +35,7 @@ struct AdamWArgs {
   void *m, *v;
   uint8_t *m_exp, *v_exp;
 };
+int adamw_vector(int bits);          // elements of a thread's vector
 void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, int hat_type, int bits, hipStream_t s);
 void launch_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, hipStream_t s);
 
@@ -92,6 +95,33 @@ __device__ __forceinline__ float to_float(bf16 x) { return __uint_as_float((uint
 template <class T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16 from_float<bf16>(float x) { return __builtin_bit_cast(bf16, (__bf16)x); }   // to nearest, ties to even
+
+// Four or eight values of T as they lie in memory, and as floats.
+template <class T, int V> struct alignas(sizeof(T) * V) Pack { T x[V]; };
+template <class T, int V> __device__ __forceinline__ void load_pack(float (&f)[V], const T* p) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * V >= 16 ? 4 : 2)));
+  constexpr int N = sizeof(T) * V / sizeof(words);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const words q = __builtin_nontemporal_load((const words*)p + i);
+    constexpr int E = V / N;
+    Pack<T, E> k = __builtin_bit_cast(Pack<T, E>, q);
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[i * E + e] = to_float(k.x[e]);
+  }
+}
+template <class T, int V> __device__ __forceinline__ void store_pack(T* p, const float (&f)[V]) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * V >= 16 ? 4 : 2)));
+  constexpr int N = sizeof(T) * V / sizeof(words);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    constexpr int E = V / N;
+    Pack<T, E> k;
+#pragma unroll
+    for (int e = 0; e < E; ++e) k.x[e] = from_float<T>(f[i * E + e]);
+    __builtin_nontemporal_store(__builtin_bit_cast(words, k), (words*)p + i);
+  }
+}
 
 // f(T{}, U{}) with the C++ types of two pb_dtype
 template <class F> void with_type(int t, F&& f) { t == PB_BF16 ? f(bf16()) : f(float()); }
