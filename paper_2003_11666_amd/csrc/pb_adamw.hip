@@ -1,4 +1,6 @@
 // AdamW over many tensors at once, moments in 32 or in 8 bits (pb_adamw_step, pb_adamw_moments).
+#include <type_traits>
+
 #include "pb_ops.h"
 
 namespace pb {
@@ -13,26 +15,33 @@ constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ULL;
 
 // 8-bit moments.  With 3 bits kept behind the leading one, an fp32 number is its bit pattern >> 20 (exponent field and three
 // bits), and a code counts these from the block's top downwards: encoding and decoding are integer shifts and sums.
+// PLAIN: the block's exponent lies in [32, 254], so that no code reaches below the smallest normal number and no value is NaN.
 constexpr int TOP_M = 15, TOP_V = 31;   // exponents below the block's that a code reaches: 4 bits of m's seven, 5 bits of v's eight
+__device__ __forceinline__ bool plain_exponent(int e) { return e > TOP_V && e < 255; }
 __device__ __forceinline__ int block_exponent(uint32_t largest) { return (int)((largest + (1u << 20)) >> 23); }
-__device__ __forceinline__ float decode_m(uint32_t code, int e) {
-  const int c = (int)(code & 127), q = c + 8 * (e - TOP_M);
-  const float x = __uint_as_float(e == 255 ? 0x7FC00000u : c == 0 || q < 0 ? 0u : (uint32_t)q << 20);
-  return code & 128 ? -x : x;
+template <int TOP, bool PLAIN> __device__ __forceinline__ uint32_t decode(uint32_t c, int e) {
+  const int q = (int)c + 8 * (e - TOP);
+  if (PLAIN) return c == 0 ? 0u : (uint32_t)q << 20;
+  return e == 255 ? 0x7FC00000u : c == 0 || q < 0 ? 0u : (uint32_t)q << 20;
 }
-__device__ __forceinline__ float decode_v(uint32_t code, int e) {
-  const int c = (int)code, q = c + 8 * (e - TOP_V);
-  return __uint_as_float(e == 255 ? 0x7FC00000u : c == 0 || q < 0 ? 0u : (uint32_t)q << 20);
+template <bool PLAIN> __device__ __forceinline__ float decode_m(uint32_t code, int e) {
+  return __uint_as_float(decode<TOP_M, PLAIN>(code & 127, e) | (code & 128) << 24);
 }
-__device__ __forceinline__ uint32_t encode_m(float x, uint32_t dither, int e) {
+template <bool PLAIN> __device__ __forceinline__ float decode_v(uint32_t code, int e) { return __uint_as_float(decode<TOP_V, PLAIN>(code, e)); }
+template <bool PLAIN> __device__ __forceinline__ uint32_t encode_m(float x, uint32_t dither, int e) {
   const uint32_t bits = __float_as_uint(x) & 0x7FFFFFFF;
-  const int c = (int)((bits + dither) >> 20) - 8 * (e - TOP_M);
-  return (bits == 0 || c < 0 ? 0u : c > 127 ? 127u : (uint32_t)c) | (x < 0.f ? 128u : 0u);
+  int c = (int)((bits + dither) >> 20) - 8 * (e - TOP_M);
+  c = c < 0 ? 0 : c > 127 ? 127 : c;
+  if (!PLAIN && bits == 0) c = 0;   // (else 0 lies below code 0 by itself)
+  return (uint32_t)c | (x < 0.f ? 128u : 0u);
 }
-__device__ __forceinline__ uint32_t encode_v(float x, uint32_t dither, int e) {
+template <bool PLAIN> __device__ __forceinline__ uint32_t encode_v(float x, uint32_t dither, int e) {
   const uint32_t bits = __float_as_uint(x);
-  const int q = (int)((bits + dither) >> 20), c = (q < 1 ? 1 : q) - 8 * (e - TOP_V);
-  return bits == 0 ? 0u : c < 1 ? 1u : c > 255 ? 255u : (uint32_t)c;
+  int q = (int)((bits + dither) >> 20);
+  if (!PLAIN) q = q < 1 ? 1 : q;
+  const int c = q - 8 * (e - TOP_V), in = c < 1 ? 1 : c > 255 ? 255 : c;
+  if (PLAIN) return min((uint32_t)in, bits);   // (0 for 0; a value whose bits are below its code has code 1)
+  return bits == 0 ? 0u : (uint32_t)in;
 }
 
 struct Coeffs { float lr, root; };   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
@@ -111,28 +120,29 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
   const Coeffs k = a.step_dev ? coeffs(a, step) : Coeffs{a.lr_t, a.root_t};
   const float gs = a.grad_scale ? *a.grad_scale : 1.f, decay = a.decay[t];
   const uint64_t key = BITS == 8 ? mix(a.seed ^ mix((uint64_t)step)) : 0;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
-    if ((i & ~(int64_t)(PB_ADAMW_BLOCK - 1)) >= n) continue;
-    float hv[V];
-    uint32_t tm = 0, tv = 0;
+  // PLAIN (8 bits): whole vectors, exponents in the range above before and after, and a quotient of which each function may be
+  // one unit off (a.approx).  The kernel is bound by its instructions otherwise: a hundred for an element with exact
+  // divisions and every case of the codes, 610 us for 243 million bf16 weights, which take 390 at the rate of memory.
+  auto update = [&](auto P, int u, float (&hv)[V], uint32_t& tm, uint32_t& tv) {
+    constexpr bool PLAIN = decltype(P)::value;
+    const int64_t i = i0 + u * AT * V;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const bool mine = i + e < n;
       float m = mv[u][e], v = vv[u][e];
       if constexpr (BITS == 8) {
-        m = decode_m(mc[u][e / 4] >> 8 * (e % 4) & 255, em[u]);
-        v = decode_v(vc[u][e / 4] >> 8 * (e % 4) & 255, ev[u]);
+        m = decode_m<PLAIN>(mc[u][e / 4] >> 8 * (e % 4) & 255, em[u]);
+        v = decode_v<PLAIN>(vc[u][e / 4] >> 8 * (e % 4) & 255, ev[u]);
       }
       const float grad = gv[u][e] * gs;
       // (each operation rounded: which code an 8-bit moment gets is defined by that)
       m = a.b1 * m + a.c1 * grad;
       v = a.b2 * v + a.c2 * (grad * grad);
-      const float d = k.lr * (m / fmaf(sqrtf(v), k.root, a.eps));
+      const float den = fmaf(PLAIN ? __builtin_amdgcn_sqrtf(v) : sqrtf(v), k.root, a.eps);
+      const float d = PLAIN ? k.lr * m * __builtin_amdgcn_rcpf(den) : k.lr * (m / den);
       const float w2 = fmaf(-decay, wv[u][e], wv[u][e]) - d;
       wv[u][e] = w2;
       hv[e] = fmaf(-a.horizon, d, w2);
+      const bool mine = PLAIN || i + e < n;
       mv[u][e] = mine ? m : 0.f;
       vv[u][e] = mine ? v : 0.f;
       if (BITS == 8) {
@@ -140,6 +150,16 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
         tv = max(tv, __float_as_uint(vv[u][e]) & 0x7FFFFFFF);
       }
     }
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
+    if ((i & ~(int64_t)(PB_ADAMW_BLOCK - 1)) >= n) continue;
+    float hv[V];
+    uint32_t tm = 0, tv = 0;
+    const bool plain = BITS == 8 && a.approx && __all(vec && i + V <= n && plain_exponent(em[u]) && plain_exponent(ev[u]));
+    if (plain) update(std::true_type(), u, hv, tm, tv);
+    else update(std::false_type(), u, hv, tm, tv);
     if (vec && i + V <= n) {
       store_pack<W, V>(w + i, wv[u]);
       if (hat) store_pack<H, V>(hat + i, hv);
@@ -166,12 +186,22 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
     } else {
       const int m_top = block_exponent(row_max(tm)), v_top = block_exponent(row_max(tv));
       uint32_t m2[2] = {0, 0}, v2[2] = {0, 0};
+      auto encode = [&](auto P) {
+        constexpr bool PLAIN = decltype(P)::value;
+        const uint64_t count = key + (uint64_t)(at >> 1) * GOLDEN;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {   // (one draw of 64 bits for two elements)
-        const uint32_t z = (uint32_t)(mix((uint64_t)((at >> 1) + e / 2) * GOLDEN + key) >> 32 * (e & 1));
-        m2[e / 4] |= encode_m(mv[u][e], (z & 0xFFFF) << 4 | 8, m_top) << 8 * (e % 4);
-        v2[e / 4] |= encode_v(vv[u][e], (z >> 16) << 4 | 8, v_top) << 8 * (e % 4);
-      }
+        for (int e = 0; e < V; e += 2) {   // (one draw of 64 bits for two elements)
+          const uint64_t z = mix(count + (uint64_t)(e / 2) * GOLDEN);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t r = (uint32_t)(z >> 32 * h);
+            m2[e / 4] |= encode_m<PLAIN>(mv[u][e + h], (r & 0xFFFF) << 4 | 8, m_top) << 8 * ((e + h) % 4);
+            v2[e / 4] |= encode_v<PLAIN>(vv[u][e + h], (r >> 12 & 0xFFFF0) | 8, v_top) << 8 * ((e + h) % 4);
+          }
+        }
+      };
+      if (__all(plain_exponent(m_top) && plain_exponent(v_top))) encode(std::true_type());
+      else encode(std::false_type());
       typedef uint32_t two __attribute__((ext_vector_type(2)));
       __builtin_nontemporal_store((two){m2[0], m2[1]}, (two*)((uint8_t*)a.m + at));
       __builtin_nontemporal_store((two){v2[0], v2[1]}, (two*)((uint8_t*)a.v + at));
@@ -185,23 +215,38 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
 
 int adamw_vector(int bits) { return bits == 8 ? 8 : 4; }
 
-// 8 codes of each moment per thread: 10 bytes an element, bound by memory.
+// 10 bytes an element, bound by memory.  A thread writes vectors of 4 floats that its neighbours continue: with 8 side by side
+// a wavefront's store leaves half of every 32 bytes to the next one, 812 us for 243 million elements.
+constexpr int MOMENTS_CHUNK = 4096;
 __global__ void __launch_bounds__(AT)
 k_adamw_moments(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v, const uint8_t* __restrict__ m_exp, const uint8_t* __restrict__ v_exp,
                 int64_t n, float* __restrict__ m_out, float* __restrict__ v_out) {
-  typedef uint32_t two __attribute__((ext_vector_type(2)));
-  const int64_t i = ((int64_t)blockIdx.x * AT + threadIdx.x) * 8;
-  if (i >= n) return;
-  const two mc = __builtin_nontemporal_load((const two*)(m + i)), vc = __builtin_nontemporal_load((const two*)(v + i));
-  const int em = m_exp[i / PB_ADAMW_BLOCK], ev = v_exp[i / PB_ADAMW_BLOCK];
-  float a[8], b[8];
+  constexpr int U = MOMENTS_CHUNK / (4 * AT);
+  const int64_t i0 = (int64_t)blockIdx.x * MOMENTS_CHUNK + threadIdx.x * 4;
+  uint32_t mc[U], vc[U];
+  int em[U], ev[U];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    a[e] = decode_m(mc[e / 4] >> 8 * (e % 4) & 255, em);
-    b[e] = decode_v(vc[e / 4] >> 8 * (e % 4) & 255, ev);
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = i0 + u * 4 * AT;
+    if (i >= n) continue;
+    mc[u] = __builtin_nontemporal_load((const uint32_t*)(m + i));
+    vc[u] = __builtin_nontemporal_load((const uint32_t*)(v + i));
+    em[u] = m_exp[i / PB_ADAMW_BLOCK];
+    ev[u] = v_exp[i / PB_ADAMW_BLOCK];
   }
-  store_pack<float, 8>(m_out + i, a);
-  store_pack<float, 8>(v_out + i, b);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = i0 + u * 4 * AT;
+    if (i >= n) continue;
+    float a[4], b[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = decode_m<false>(mc[u] >> 8 * e & 255, em[u]);
+      b[e] = decode_v<false>(vc[u] >> 8 * e & 255, ev[u]);
+    }
+    store_pack<float, 4>(m_out + i, a);
+    store_pack<float, 4>(v_out + i, b);
+  }
 }
 
 void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, int hat_type, int bits, hipStream_t s) {
@@ -212,7 +257,7 @@ void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, in
 }
 
 void launch_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, hipStream_t s) {
-  hipLaunchKernelGGL(k_adamw_moments, dim3((unsigned)((n + 8 * AT - 1) / (8 * AT))), dim3(AT), 0, s, m, v, m_exp, v_exp, n, m_out, v_out);
+  hipLaunchKernelGGL(k_adamw_moments, dim3((unsigned)((n + MOMENTS_CHUNK - 1) / MOMENTS_CHUNK)), dim3(AT), 0, s, m, v, m_exp, v_exp, n, m_out, v_out);
 }
 
 }  // namespace pb

@@ -74,6 +74,8 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   a.eps = (float)d->eps; a.horizon = (float)d->horizon;
   a.lr = d->lr; a.beta1 = d->beta1; a.beta2 = d->beta2;
   a.step = d->step; a.step_dev = d->step_dev; a.grad_scale = d->grad_scale; a.seed = d->seed;
+  // (the square root of a v below 2^-126 may come out as 0: at most 2^-63 / sqrt(1 - beta2) beside eps, 2^-26 of it at most)
+  a.approx = a.eps * sqrt(1.0 - d->beta2) >= 0x1p-37;
   if (!d->step_dev) {
     a.lr_t = (float)(d->lr / (1.0 - pow(d->beta1, (double)d->step)));
     a.root_t = (float)(1.0 / sqrt(1.0 - pow(d->beta2, (double)d->step)));

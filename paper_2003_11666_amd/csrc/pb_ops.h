@@ -28,6 +28,7 @@ struct AdamWArgs {
   float b1, c1, b2, c2, eps, horizon;  // c = 1 - b
   float lr_t, root_t;                  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t): of the step on the host
   double lr, beta1, beta2;
+  int32_t approx;                      // 1: eps hides what a square root below 2^-63 may lose in the hardware's own function
   int64_t step;
   const int64_t* step_dev;
   const float* grad_scale;
