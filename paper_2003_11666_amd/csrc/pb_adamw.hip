@@ -75,119 +75,154 @@ static_assert(PB_ADAMW_BLOCK == 128, "16 lanes of 8 elements");
 
 constexpr int AT = 256;   // threads per workgroup
 
-// Bound by memory: 24 bytes an element with 32-bit moments, weights and gradients.  A thread takes vectors of V elements, 16
-// bytes of the 32-bit arrays or of bf16 with 8-bit moments, and requests all of its U vectors before it uses the first; the
-// arrays are passed over once per step, so every access carries the non-temporal hint.
-template <class W, class G, class H, int BITS>
+// What a thread requests for one of its vectors.
+template <class W, class G, int BITS, int V> struct Vector;
+template <class W, class G, int V> struct Vector<W, G, 32, V> {
+  Vec<W, V> w;
+  Vec<G, V> g;
+  Vec<float, V> m, v;
+  __device__ __forceinline__ void moments(const AdamWArgs& a, int64_t at) {
+    m.load((const float*)a.m + at);
+    v.load((const float*)a.v + at);
+  }
+};
+template <class W, class G, int V> struct Vector<W, G, 8, V> {
+  Vec<W, V> w;
+  Vec<G, V> g;
+  Vec<uint8_t, V> m, v;
+  int em, ev;
+  __device__ __forceinline__ void moments(const AdamWArgs& a, int64_t at) {
+    m.load((const uint8_t*)a.m + at);
+    v.load((const uint8_t*)a.v + at);
+    em = a.m_exp[at / PB_ADAMW_BLOCK];
+    ev = a.v_exp[at / PB_ADAMW_BLOCK];
+  }
+};
+
+// A thread takes U vectors of V elements -- 16 bytes of the 32-bit arrays, or of bf16 with 8-bit moments -- and has the next A
+// of them under way; the arrays are passed over once per step, so every access carries the non-temporal hint.  With 32-bit
+// moments it is bound by memory (24 bytes an element) and requests all it needs at once.  With 8-bit moments it is bound by
+// its instructions as much.
+template <class W, class G, class H, int BITS, int CHUNK>
 __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
-  constexpr int V = BITS == 8 ? 8 : 4, U = ADAMW_CHUNK / (AT * V);
+  constexpr int V = BITS == 8 ? 8 : 4, U = CHUNK / (AT * V), A = BITS == 8 ? 2 : U;
   const int t = tensor_of(a, (int)blockIdx.x);
-  const int64_t n = a.n[t], i0 = (int64_t)((int)blockIdx.x - a.first[t]) * ADAMW_CHUNK + threadIdx.x * V;
+  const int64_t n = a.n[t], i0 = (int64_t)((int)blockIdx.x - a.first[t]) * CHUNK + threadIdx.x * V;
   const bool vec = a.vec[t];
   W* w = (W*)a.w[t];
   const G* g = (const G*)a.g[t];
   H* hat = (H*)a.hat[t];
   const int64_t at0 = a.at[t] + i0;
-  float wv[U][V], gv[U][V], mv[U][V], vv[U][V];
-  uint32_t mc[U][2], vc[U][2];
-  int em[U], ev[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
-    if ((i & ~(int64_t)(PB_ADAMW_BLOCK - 1)) >= n) continue;   // (whole blocks: their lanes take the maximum together)
+  Vector<W, G, BITS, V> x[A];
+  // (whole blocks of moments: their lanes take the maximum together, and entries up to the next multiple of a block belong to the tensor)
+  auto inside = [&](int u) { return ((i0 + u * AT * V) & ~(int64_t)(PB_ADAMW_BLOCK - 1)) < n; };
+  auto request = [&](Vector<W, G, BITS, V>& y, int u) {
+    const int64_t i = i0 + u * AT * V;
+    if (!inside(u)) return;
     if (vec && i + V <= n) {
-      load_pack<W, V>(wv[u], w + i);
-      load_pack<G, V>(gv[u], g + i);
+      y.w.load(w + i);
+      y.g.load(g + i);
     } else {
+      float wf[V], gf[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        wv[u][e] = i + e < n ? to_float(w[i + e]) : 0.f;
-        gv[u][e] = i + e < n ? to_float(g[i + e]) : 0.f;
+        wf[e] = i + e < n ? to_float(w[i + e]) : 0.f;
+        gf[e] = i + e < n ? to_float(g[i + e]) : 0.f;
       }
+      y.w.put(wf);
+      y.g.put(gf);
     }
-    if constexpr (BITS == 32) {   // (entries up to the next multiple of a block belong to the tensor)
-      load_pack<float, V>(mv[u], (const float*)a.m + at);
-      load_pack<float, V>(vv[u], (const float*)a.v + at);
-    } else {
-      typedef uint32_t two __attribute__((ext_vector_type(2)));
-      const two m2 = __builtin_nontemporal_load((const two*)((const uint8_t*)a.m + at)), v2 = __builtin_nontemporal_load((const two*)((const uint8_t*)a.v + at));
-      mc[u][0] = m2.x; mc[u][1] = m2.y; vc[u][0] = v2.x; vc[u][1] = v2.y;
-      em[u] = a.m_exp[at / PB_ADAMW_BLOCK];
-      ev[u] = a.v_exp[at / PB_ADAMW_BLOCK];
-    }
-  }
+    y.moments(a, at0 + u * AT * V);
+  };
+#pragma unroll
+  for (int u = 0; u < A; ++u) request(x[u], u);
   const int64_t step = a.step_dev ? *a.step_dev : a.step;
   const Coeffs k = a.step_dev ? coeffs(a, step) : Coeffs{a.lr_t, a.root_t};
   const float gs = a.grad_scale ? *a.grad_scale : 1.f, decay = a.decay[t];
   const uint64_t key = BITS == 8 ? mix(a.seed ^ mix((uint64_t)step)) : 0;
+  float wv[V], mv[V], vv[V], hv[V];
+  uint32_t tm, tv;
   // PLAIN (8 bits): whole vectors, exponents in the range above before and after, and a quotient of which each function may be
-  // one unit off (a.approx).  The kernel is bound by its instructions otherwise: a hundred for an element with exact
-  // divisions and every case of the codes, 610 us for 243 million bf16 weights, which take 390 at the rate of memory.
-  auto update = [&](auto P, int u, float (&hv)[V], uint32_t& tm, uint32_t& tv) {
+  // one unit off (a.approx).  With exact divisions and every case of the codes an element takes a hundred instructions, 610
+  // us for 243 million bf16 weights, which take 390 at the rate of memory.
+  auto update = [&](auto P, const Vector<W, G, BITS, V>& y, int u) {
     constexpr bool PLAIN = decltype(P)::value;
     const int64_t i = i0 + u * AT * V;
+    tm = tv = 0;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      float m = mv[u][e], v = vv[u][e];
+      float m, v;
       if constexpr (BITS == 8) {
-        m = decode_m<PLAIN>(mc[u][e / 4] >> 8 * (e % 4) & 255, em[u]);
-        v = decode_v<PLAIN>(vc[u][e / 4] >> 8 * (e % 4) & 255, ev[u]);
+        m = decode_m<PLAIN>(y.m.q[0][e / 4] >> 8 * (e % 4) & 255, y.em);
+        v = decode_v<PLAIN>(y.v.q[0][e / 4] >> 8 * (e % 4) & 255, y.ev);
+      } else {
+        m = y.m.get(e);
+        v = y.v.get(e);
       }
-      const float grad = gv[u][e] * gs;
+      const float grad = y.g.get(e) * gs, w1 = y.w.get(e);
       // (each operation rounded: which code an 8-bit moment gets is defined by that)
       m = a.b1 * m + a.c1 * grad;
       v = a.b2 * v + a.c2 * (grad * grad);
       const float den = fmaf(PLAIN ? __builtin_amdgcn_sqrtf(v) : sqrtf(v), k.root, a.eps);
       const float d = PLAIN ? k.lr * m * __builtin_amdgcn_rcpf(den) : k.lr * (m / den);
-      const float w2 = fmaf(-decay, wv[u][e], wv[u][e]) - d;
-      wv[u][e] = w2;
-      hv[e] = fmaf(-a.horizon, d, w2);
+      wv[e] = fmaf(-decay, w1, w1) - d;
+      hv[e] = fmaf(-a.horizon, d, wv[e]);
       const bool mine = PLAIN || i + e < n;
-      mv[u][e] = mine ? m : 0.f;
-      vv[u][e] = mine ? v : 0.f;
+      mv[e] = mine ? m : 0.f;
+      vv[e] = mine ? v : 0.f;
       if (BITS == 8) {
-        tm = max(tm, __float_as_uint(mv[u][e]) & 0x7FFFFFFF);
-        tv = max(tv, __float_as_uint(vv[u][e]) & 0x7FFFFFFF);
+        tm = max(tm, __float_as_uint(mv[e]) & 0x7FFFFFFF);
+        tv = max(tv, __float_as_uint(vv[e]) & 0x7FFFFFFF);
       }
     }
   };
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
-    if ((i & ~(int64_t)(PB_ADAMW_BLOCK - 1)) >= n) continue;
-    float hv[V];
-    uint32_t tm = 0, tv = 0;
-    const bool plain = BITS == 8 && a.approx && __all(vec && i + V <= n && plain_exponent(em[u]) && plain_exponent(ev[u]));
-    if (plain) update(std::true_type(), u, hv, tm, tv);
-    else update(std::false_type(), u, hv, tm, tv);
+    if (!inside(u)) continue;
+    bool plain = false;
+    if constexpr (BITS == 8) plain = a.approx && __all(vec && i + V <= n && plain_exponent(x[u % A].em) && plain_exponent(x[u % A].ev));
+    if (BITS == 8 && plain) update(std::true_type(), x[u % A], u);
+    else update(std::false_type(), x[u % A], u);
+    if (u + A < U) request(x[u % A], u + A);
     if (vec && i + V <= n) {
-      store_pack<W, V>(w + i, wv[u]);
-      if (hat) store_pack<H, V>(hat + i, hv);
+      Vec<W, V> q;
+      q.put(wv);
+      q.store(w + i);
+      if (hat) {
+        Vec<H, V> r;
+        r.put(hv);
+        r.store(hat + i);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         if (i + e >= n) continue;
-        w[i + e] = from_float<W>(wv[u][e]);
+        w[i + e] = from_float<W>(wv[e]);
         if (hat) hat[i + e] = from_float<H>(hv[e]);
       }
     }
     if constexpr (BITS == 32) {
       if (i + V <= n) {
-        store_pack<float, V>((float*)a.m + at, mv[u]);
-        store_pack<float, V>((float*)a.v + at, vv[u]);
+        Vec<float, V> q;
+        q.put(mv);
+        q.store((float*)a.m + at);
+        q.put(vv);
+        q.store((float*)a.v + at);
       } else {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           if (i + e >= n) continue;
-          ((float*)a.m)[at + e] = mv[u][e];
-          ((float*)a.v)[at + e] = vv[u][e];
+          ((float*)a.m)[at + e] = mv[e];
+          ((float*)a.v)[at + e] = vv[e];
         }
       }
     } else {
       const int m_top = block_exponent(row_max(tm)), v_top = block_exponent(row_max(tv));
-      uint32_t m2[2] = {0, 0}, v2[2] = {0, 0};
+      Vec<uint8_t, V> mq, vq;
       auto encode = [&](auto P) {
         constexpr bool PLAIN = decltype(P)::value;
+        uint32_t m2[2] = {0, 0}, v2[2] = {0, 0};
         const uint64_t count = key + (uint64_t)(at >> 1) * GOLDEN;
 #pragma unroll
         for (int e = 0; e < V; e += 2) {   // (one draw of 64 bits for two elements)
@@ -195,16 +230,16 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint32_t r = (uint32_t)(z >> 32 * h);
-            m2[e / 4] |= encode_m<PLAIN>(mv[u][e + h], (r & 0xFFFF) << 4 | 8, m_top) << 8 * ((e + h) % 4);
-            v2[e / 4] |= encode_v<PLAIN>(vv[u][e + h], (r >> 12 & 0xFFFF0) | 8, v_top) << 8 * ((e + h) % 4);
+            m2[e / 4] |= encode_m<PLAIN>(mv[e + h], (r & 0xFFFF) << 4 | 8, m_top) << 8 * ((e + h) % 4);
+            v2[e / 4] |= encode_v<PLAIN>(vv[e + h], (r >> 12 & 0xFFFF0) | 8, v_top) << 8 * ((e + h) % 4);
           }
         }
+        mq.q[0][0] = m2[0]; mq.q[0][1] = m2[1]; vq.q[0][0] = v2[0]; vq.q[0][1] = v2[1];
       };
       if (__all(plain_exponent(m_top) && plain_exponent(v_top))) encode(std::true_type());
       else encode(std::false_type());
-      typedef uint32_t two __attribute__((ext_vector_type(2)));
-      __builtin_nontemporal_store((two){m2[0], m2[1]}, (two*)((uint8_t*)a.m + at));
-      __builtin_nontemporal_store((two){v2[0], v2[1]}, (two*)((uint8_t*)a.v + at));
+      mq.store((uint8_t*)a.m + at);
+      vq.store((uint8_t*)a.v + at);
       if ((threadIdx.x & 15) == 0) {
         a.m_exp[at / PB_ADAMW_BLOCK] = (uint8_t)m_top;
         a.v_exp[at / PB_ADAMW_BLOCK] = (uint8_t)v_top;
@@ -244,15 +279,19 @@ k_adamw_moments(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v, co
       a[e] = decode_m<false>(mc[u] >> 8 * e & 255, em[u]);
       b[e] = decode_v<false>(vc[u] >> 8 * e & 255, ev[u]);
     }
-    store_pack<float, 4>(m_out + i, a);
-    store_pack<float, 4>(v_out + i, b);
+    Vec<float, 4> q;
+    q.put(a);
+    q.store(m_out + i);
+    q.put(b);
+    q.store(v_out + i);
   }
 }
 
-void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, int hat_type, int bits, hipStream_t s) {
+void launch_adamw(const AdamWArgs& a, int64_t groups, int chunk, int w_type, int g_type, int hat_type, int bits, hipStream_t s) {
   with_type(w_type, [&](auto w) { with_type(g_type, [&](auto g) { with_type(hat_type, [&](auto h) {
-    if (bits == 32) hipLaunchKernelGGL((k_adamw<decltype(w), decltype(g), decltype(h), 32>), dim3((unsigned)groups), dim3(AT), 0, s, a);
-    else hipLaunchKernelGGL((k_adamw<decltype(w), decltype(g), decltype(h), 8>), dim3((unsigned)groups), dim3(AT), 0, s, a);
+    using W = decltype(w); using G = decltype(g); using H = decltype(h);
+    auto f = bits == 32 ? k_adamw<W, G, H, 32, 4096> : chunk == 8192 ? k_adamw<W, G, H, 8, 8192> : k_adamw<W, G, H, 8, 4096>;
+    hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(AT), 0, s, a);
   }); }); });
 }
 

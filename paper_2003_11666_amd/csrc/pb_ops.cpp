@@ -81,9 +81,10 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
     a.root_t = (float)(1.0 / sqrt(1.0 - pow(d->beta2, (double)d->step)));
   }
   a.m = m; a.v = v; a.m_exp = m_exp; a.v_exp = v_exp;
+  const int chunk = adamw_chunk(d->moment_bits, blocks * PB_ADAMW_BLOCK);
   int64_t at = 0, groups = 0;
   auto launch = [&] {
-    launch_adamw(a, groups, d->w_type, d->g_type, d->w_hat_type, d->moment_bits, (hipStream_t)stream);
+    launch_adamw(a, groups, chunk, d->w_type, d->g_type, d->w_hat_type, d->moment_bits, (hipStream_t)stream);
     a.n_tensors = 0;
     groups = 0;
     return launched();
@@ -91,7 +92,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   for (int32_t i = 0; i < n_tensors; ++i) {
     const pb_adamw_tensor& t = ts[i];
     if (t.n == 0) continue;
-    const int64_t g = (t.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+    const int64_t g = (t.n + chunk - 1) / chunk;
     if (g > 0x7fffffff) return fail(PB_E_INVALID, "tensor %d is too large", (int)i);
     if (a.n_tensors == ADAMW_TENSORS || groups + g > 0x7fffffff) {
       const int rc = launch();

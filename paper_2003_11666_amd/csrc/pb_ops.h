@@ -13,7 +13,10 @@ int fail(int code, const char* fmt, ...);   // pb_host.cpp: the text of pb_last_
 
 // ------------------------------------------------------------------------------------------------ AdamW (pb_adamw.hip)
 constexpr int ADAMW_TENSORS = 64;    // tensors per launch: a lane each in the search for a workgroup's tensor, 3 KB of arguments
-constexpr int ADAMW_CHUNK = 4096;    // elements per workgroup
+// Elements per workgroup.  8-bit moments: a workgroup that goes on to more vectors has their requests under way while it
+// computes (243 million bf16 weights 540 -> 487 us), but 8192 elements are too many where the chip holds all workgroups in two
+// or three rounds (17 million fp32 weights 57 -> 61 us).
+constexpr int adamw_chunk(int bits, int64_t elements) { return bits == 8 && elements >= (int64_t)1 << 26 ? 8192 : 4096; }
 
 struct AdamWArgs {
   void* w[ADAMW_TENSORS];
@@ -37,7 +40,7 @@ struct AdamWArgs {
   uint8_t *m_exp, *v_exp;
 };
 int adamw_vector(int bits);          // elements of a thread's vector
-void launch_adamw(const AdamWArgs& a, int64_t groups, int w_type, int g_type, int hat_type, int bits, hipStream_t s);
+void launch_adamw(const AdamWArgs& a, int64_t groups, int chunk, int w_type, int g_type, int hat_type, int bits, hipStream_t s);
 void launch_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, hipStream_t s);
 
 // ------------------------------------------------------------------------------------ log probabilities (pb_logprob.hip)
@@ -97,32 +100,34 @@ template <class T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16 from_float<bf16>(float x) { return __builtin_bit_cast(bf16, (__bf16)x); }   // to nearest, ties to even
 
-// Four or eight values of T as they lie in memory, and as floats.
-template <class T, int V> struct alignas(sizeof(T) * V) Pack { T x[V]; };
-template <class T, int V> __device__ __forceinline__ void load_pack(float (&f)[V], const T* p) {
+// V values of T in a row, 8 bytes of them or more: as they come from memory in 16-byte (8-byte) requests, and as floats.
+template <class T, int V> struct Vec {
   typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * V >= 16 ? 4 : 2)));
-  constexpr int N = sizeof(T) * V / sizeof(words);
+  static constexpr int N = sizeof(T) * V / sizeof(words), E = V / N;
+  struct alignas(sizeof(words)) Pack { T x[E]; };
+  words q[N];
+  __device__ __forceinline__ void load(const T* p) {   // (NT: passed over once)
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const words q = __builtin_nontemporal_load((const words*)p + i);
-    constexpr int E = V / N;
-    Pack<T, E> k = __builtin_bit_cast(Pack<T, E>, q);
-#pragma unroll
-    for (int e = 0; e < E; ++e) f[i * E + e] = to_float(k.x[e]);
+    for (int i = 0; i < N; ++i) q[i] = __builtin_nontemporal_load((const words*)p + i);
   }
-}
-template <class T, int V> __device__ __forceinline__ void store_pack(T* p, const float (&f)[V]) {
-  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * V >= 16 ? 4 : 2)));
-  constexpr int N = sizeof(T) * V / sizeof(words);
+  __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    constexpr int E = V / N;
-    Pack<T, E> k;
-#pragma unroll
-    for (int e = 0; e < E; ++e) k.x[e] = from_float<T>(f[i * E + e]);
-    __builtin_nontemporal_store(__builtin_bit_cast(words, k), (words*)p + i);
+    for (int i = 0; i < N; ++i) __builtin_nontemporal_store(q[i], (words*)p + i);
   }
-}
+  __device__ __forceinline__ float get(int e) const {
+    const uint32_t w = q[e / E][e % E * sizeof(T) / 4];
+    return __uint_as_float(sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
+  }
+  __device__ __forceinline__ void put(const float (&f)[V]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      Pack k;
+#pragma unroll
+      for (int e = 0; e < E; ++e) k.x[e] = from_float<T>(f[i * E + e]);
+      q[i] = __builtin_bit_cast(words, k);
+    }
+  }
+};
 
 // f(T{}, U{}) with the C++ types of two pb_dtype
 template <class F> void with_type(int t, F&& f) { t == PB_BF16 ? f(bf16()) : f(float()); }
