@@ -1,111 +1,333 @@
 // Log probabilities of given tokens, entropies, top alternatives (pb_log_probs) and their gradient (pb_log_probs_backward).
 #include <math.h>
 
+#include <type_traits>
+
 #include "pb_ops.h"
+#include "pb_wave.h"
 
 namespace pb {
 
-constexpr int LB = 256;   // threads per workgroup
+constexpr int LB = 256;             // threads per workgroup: 4 wavefronts
+constexpr int WAVES = LB / 64;
+constexpr int64_t SHORT_ROW = 2048; // rows up to here are a wavefront's each
+constexpr float LOG2E = 1.44269504088896340736f;
 
-// Order of the alternatives: a larger key is a better one.  High half: the logit as an unsigned number that rises with it (both
-// zeros the same, a NaN above all), low half: the index, lower ones first.  0 and all ones are no keys.
+// 16 bytes of logits, on a boundary of one logit: rows start anywhere.
+template <class T> struct Sixteen {
+  typedef uint32_t words __attribute__((ext_vector_type(4)));
+  typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
+  static constexpr int V = 16 / sizeof(T);
+  words q;
+  __device__ __forceinline__ void load(const T* p) { q = __builtin_nontemporal_load((const loose*)p); }
+  __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store((loose)q, (loose*)p); }
+  __device__ __forceinline__ float get(int e) const {
+    const uint32_t w = q[e * sizeof(T) / 4];
+    return __uint_as_float(sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
+  }
+  __device__ __forceinline__ void put(const float (&f)[V]) {
+    struct alignas(16) { T x[V]; } k;
+#pragma unroll
+    for (int e = 0; e < V; ++e) k.x[e] = from_float<T>(f[e]);
+    q = __builtin_bit_cast(words, k);
+  }
+};
+
+// ------------------------------------------------------------------------------------------------------- running sums
+// Of the logits seen so far: maximum m, s = sum e^(x - m), u = sum (x - m) e^(x - m), passed over once.  -inf as maximum stands
+// for none that counts; a NaN, or +inf, makes s NaN.  (x - m is held above -150 in u, whose term is 0 from there on: 0 * -inf.)
+struct Sums { float m, s, u; };
+constexpr Sums NOTHING = {-INFINITY, 0.f, 0.f};
+__device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.f : m; }
+
+// the same sums against the maximum `to` >= m
+__device__ __forceinline__ void rescale(Sums& a, float to) {
+  const float ref = against(to), d = fmaxf(a.m - ref, -200.f), c = __builtin_amdgcn_exp2f(d * LOG2E);
+  a.u = c * fmaf(d, a.s, a.u);
+  a.s *= c;
+  a.m = to;
+}
+
+template <int N> __device__ __forceinline__ void take(Sums& a, const float (&x)[N]) {
+  float m = a.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+  rescale(a, m);
+  const float ref = against(m);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = x[i] - ref, e = __builtin_amdgcn_exp2f(d * LOG2E);
+    a.s += e;
+    a.u = fmaf(e, fmaxf(d, -150.f), a.u);
+  }
+}
+
+__device__ __forceinline__ void join_lanes(Sums& a) {
+  rescale(a, wave_max_dpp(a.m));
+  a.s = wave_sum(a.s);
+  a.u = wave_sum(a.u);
+}
+
+// ------------------------------------------------------------------------------------------------------ alternatives
+// Their order: a larger key is a better one.  High half: the logit as an unsigned number that rises with it (both zeros the
+// same, a NaN above all), low half: the index, lower ones first.  0 is no key.
 __device__ __forceinline__ uint64_t top_key(float x, uint32_t i) {
   const uint32_t b = __float_as_uint(x + 0.f);
   const uint32_t o = x != x ? 0xFFFFFFFEu : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
   return (uint64_t)o << 32 | (uint32_t)~i;
 }
-
-template <class T, class OP>
-__device__ T reduce(T x, T* lds, OP op) {
-  lds[threadIdx.x] = x;
-  __syncthreads();
-  for (int s = LB / 2; s > 0; s >>= 1) {
-    if ((int)threadIdx.x < s) lds[threadIdx.x] = op(lds[threadIdx.x], lds[threadIdx.x + s]);
-    __syncthreads();
-  }
-  const T r = lds[0];
-  __syncthreads();
-  return r;
+__device__ __forceinline__ float key_logit(uint64_t k) {   // NaN of no key
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o);
+}
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
 }
 
-template <class T, class ID>
-__global__ void __launch_bounds__(LB) k_logp(const LogpArgs a) {
-  __shared__ float f[LB];
-  __shared__ uint64_t u[LB];
-  const int64_t r = blockIdx.x;
-  const T* x = (const T*)a.logits + r * a.stride;
-  float m = -INFINITY;
-  for (int64_t j = threadIdx.x; j < a.vocab; j += LB) m = fmaxf(m, to_float(x[j]) * a.scale);
-  m = reduce(m, f, [](float p, float q) { return fmaxf(p, q); });
-  const float ref = m == -INFINITY ? 0.f : m;
-  float s = 0.f, h = 0.f;
-  for (int64_t j = threadIdx.x; j < a.vocab; j += LB) {
-    const float d = to_float(x[j]) * a.scale - ref, e = expf(d);
-    s += e;
-    h += e * fmaxf(d, -150.f);
+// The best keys that a wavefront has seen, in falling order, one in each lane; a key enters if it beats the `top`-th.  Few do:
+// of n keys in no order about top * ln(n / top), each of which costs some twenty instructions.
+struct Best {
+  uint64_t key = 0, bar = 0;   // the lane's key; the top-th of all
+  float bar_logit;             // a logit below it cannot enter (NaN: any can)
+  int top;
+  __device__ __forceinline__ Best(int top) : bar_logit(key_logit(0)), top(top) {}
+  __device__ __forceinline__ void enter(uint64_t k) {   // of every lane; 0 for none
+    const int lane = threadIdx.x & 63;
+    for (uint64_t more = __ballot(k > bar); more; more &= __ballot(k > bar)) {
+      const int from = __builtin_ctzll(more);
+      const uint64_t x = lane_of(k, from);
+      const int place = __popcll(__ballot(key > x));
+      const uint64_t left = (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(key >> 32), 0x138, 0xF, 0xF, false) << 32 |
+                            (uint32_t)__builtin_amdgcn_update_dpp(0, (int)key, 0x138, 0xF, 0xF, false);   // of the lane before
+      key = lane < place ? key : lane == place ? x : left;
+      bar = lane_of(key, top - 1);
+      more &= ~(1ull << from);
+    }
+    bar_logit = key_logit(bar);
   }
-  s = reduce(s, f, [](float p, float q) { return p + q; });
-  h = reduce(h, f, [](float p, float q) { return p + q; });
-  const bool empty = m == -INFINITY && s == 0.f;
-  const float ls = empty ? 0.f : logf(s);
-  if (threadIdx.x == 0) {
-    a.norm[2 * r] = s != s ? s : m;
+};
+
+// -------------------------------------------------------------------------------------------------------- one stretch
+// Logits [lo, hi) of a row by `waves` wavefronts, of which this is number `wave`.
+template <class T, bool TOP>
+__device__ __forceinline__ void scan(const T* x, uint32_t lo, uint32_t hi, uint32_t wave, uint32_t waves, float scale, Sums& a, Best& best) {
+  constexpr uint32_t V = Sixteen<T>::V, U = 4;   // four requests of a lane under way
+  const uint32_t lane = threadIdx.x & 63, whole = lo + (hi - lo) / V * V;
+  for (uint32_t j0 = lo + (wave * 64 + lane) * V; j0 - lane * V < whole; j0 += U * waves * 64 * V) {
+    Sixteen<T> q[U];
+#pragma unroll
+    for (uint32_t i = 0; i < U; ++i) {
+      const uint32_t j = j0 + i * waves * 64 * V;
+      if (j < whole) q[i].load(x + j);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < U; ++i) {
+      const uint32_t j = j0 + i * waves * 64 * V;
+      if (j - lane * V >= whole) break;
+      const bool mine = j < whole;
+      float y[V];
+      bool high = false;
+#pragma unroll
+      for (uint32_t e = 0; e < V; ++e) {
+        const float z = mine ? q[i].get(e) : -INFINITY;
+        if (TOP) high |= mine && !(z < best.bar_logit);
+        y[e] = z * scale;
+      }
+      take(a, y);
+      if (TOP && __any(high)) {
+#pragma unroll
+        for (uint32_t e = 0; e < V; ++e) {
+          const float z = q[i].get(e);
+          const bool may = mine && !(z < best.bar_logit);
+          if (__any(may)) best.enter(may ? top_key(z, j + e) : 0);
+        }
+      }
+    }
+  }
+  if (whole < hi && wave == 0) {   // what no vector holds
+    const bool mine = whole + lane < hi;
+    const float z = mine ? to_float(x[whole + lane]) : -INFINITY;
+    const float y[1] = {z * scale};
+    take(a, y);
+    if (TOP) best.enter(mine ? top_key(z, whole + lane) : 0);
+  }
+}
+
+// The results of a row, by one wavefront that holds its sums and alternatives.
+template <class T, class ID>
+__device__ __forceinline__ void give(const LogpArgs& a, int64_t r, const Sums& w, const Best& best) {
+  const int lane = threadIdx.x & 63;
+  const bool empty = w.m == -INFINITY && w.s == 0.f;
+  const float ls = empty ? 0.f : logf(w.s), ref = against(w.m);
+  if (lane == 0) {
+    a.norm[2 * r] = w.s != w.s ? w.s : w.m;
     a.norm[2 * r + 1] = ls;
-    if (a.entropy) a.entropy[r] = empty ? 0.f : ls - h / s;
+    if (a.entropy) a.entropy[r] = empty ? 0.f : ls - w.u / w.s;
     if (a.logp) {
       const int64_t t = ((const ID*)a.targets)[r];
-      a.logp[r] = t >= 0 && t < a.vocab ? to_float(x[t]) * a.scale - ref - ls : 0.f;
+      a.logp[r] = t >= 0 && t < a.vocab ? to_float(((const T*)a.logits)[r * a.stride + t]) * a.scale - ref - ls : 0.f;
     }
   }
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {
-    uint64_t best = 0;
-    for (int64_t j = threadIdx.x; j < a.vocab; j += LB) {
-      const uint64_t key = top_key(to_float(x[j]), (uint32_t)j);
-      if (key < last && key > best) best = key;
-    }
-    last = reduce(best, u, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-    if (threadIdx.x == 0) {
-      const uint32_t j = ~(uint32_t)last;
-      ((ID*)a.top_ids)[r * a.top + k] = (ID)j;
-      a.top_logp[r * a.top + k] = to_float(x[j]) * a.scale - ref - ls;
+  if (lane < a.top) {
+    ((ID*)a.top_ids)[r * a.top + lane] = (ID)(uint32_t)~(uint32_t)best.key;
+    a.top_logp[r * a.top + lane] = key_logit(best.key) * a.scale - ref - ls;
+  }
+}
+
+// Of the workgroup's wavefronts into the first one.
+struct JoinLds { Sums w[WAVES]; uint64_t key[WAVES][64]; };
+template <bool TOP> __device__ __forceinline__ void join_waves(Sums& a, Best& best, JoinLds& lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  join_lanes(a);
+  if (lane == 0) lds.w[wave] = a;
+  if (TOP) lds.key[wave][lane] = best.key;
+  __syncthreads();
+  if (wave) return;
+  a = lane < WAVES ? lds.w[lane] : NOTHING;
+  join_lanes(a);
+  if (TOP)
+    for (int i = 1; i < WAVES; ++i) best.enter(lane < best.top ? lds.key[i][lane] : 0);
+}
+
+// What a workgroup that takes a part of a row leaves for the one that joins them: its sums, then its alternatives.
+__host__ __device__ __forceinline__ size_t part_bytes(int top) { return 16 + 8 * (size_t)top; }
+
+// Bound by memory: a row is read once.  A row to a wavefront (short ones), to a workgroup, or in `parts` of `part` logits to a
+// workgroup each.
+template <class T, class ID, bool TOP, bool SHORT>
+__global__ void __launch_bounds__(LB) k_logp(const LogpArgs a, int parts, int part) {
+  __shared__ JoinLds lds;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t r = SHORT ? (int64_t)blockIdx.x * WAVES + wave : blockIdx.x / parts;
+  if (SHORT && r >= a.rows) return;
+  const T* x = (const T*)a.logits + r * a.stride;
+  Sums w = NOTHING;
+  Best best(a.top);
+  if (SHORT) {
+    scan<T, TOP>(x, 0, (uint32_t)a.vocab, 0, 1, a.scale, w, best);
+    join_lanes(w);
+    give<T, ID>(a, r, w, best);
+    return;
+  }
+  const int64_t lo = (int64_t)(blockIdx.x % parts) * part;
+  scan<T, TOP>(x, (uint32_t)lo, (uint32_t)(a.vocab - lo < part ? a.vocab : lo + part), wave, WAVES, a.scale, w, best);
+  join_waves<TOP>(w, best, lds);
+  if (wave) return;
+  if (parts == 1) {
+    give<T, ID>(a, r, w, best);
+    return;
+  }
+  char* at = (char*)a.workspace + blockIdx.x * part_bytes(a.top);
+  if (lane == 0) *(Sums*)at = w;
+  if (TOP && lane < a.top) ((uint64_t*)(at + 16))[lane] = best.key;
+}
+
+template <class T, class ID, bool TOP>
+__global__ void __launch_bounds__(LB) k_logp_join(const LogpArgs a, int parts) {
+  __shared__ JoinLds lds;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t r = blockIdx.x;
+  const size_t bytes = part_bytes(a.top);
+  const char* at = (const char*)a.workspace + r * parts * bytes;
+  Sums w = NOTHING;
+  Best best(a.top);
+  for (int i = threadIdx.x; i < parts; i += LB) {
+    Sums p = *(const Sums*)(at + i * bytes);
+    const float m = fmaxf(w.m, p.m);
+    rescale(w, m);
+    rescale(p, m);
+    w.s += p.s;
+    w.u += p.u;
+  }
+  if (TOP)   // (a part's best first: the rest seldom enters)
+    for (int k = 0; k < a.top; ++k)
+      for (int i0 = wave * 64; i0 < parts; i0 += LB) best.enter(i0 + lane < parts ? ((const uint64_t*)(at + (i0 + lane) * bytes + 16))[k] : 0);
+  join_waves<TOP>(w, best, lds);
+  if (wave == 0) give<T, ID>(a, r, w, best);
+}
+
+// ----------------------------------------------------------------------------------------------------------- gradient
+// Bound by memory: each logit read and its gradient written once.  A wavefront takes U vectors of 16 bytes a lane of one row, whose
+// numbers are the same for all of its lanes.
+template <class T, class ID, bool ENT>
+__global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t pieces, int per_row) {
+  constexpr int V = Sixteen<T>::V, U = 4, PIECE = 64 * V * U;
+  const int lane = threadIdx.x & 63;
+  for (int64_t p = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); p < pieces; p += (int64_t)gridDim.x * WAVES) {
+    const int64_t r = p / per_row;
+    const uint32_t vocab = (uint32_t)a.vocab, j0 = (uint32_t)(p - r * per_row) * PIECE + lane * V;
+    const T* x = (const T*)a.logits + r * a.stride;
+    T* d = (T*)a.d + r * a.d_stride;
+    Sixteen<T> q[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (j0 + (i * 64 + 1) * V <= vocab) q[i].load(x + j0 + i * 64 * V);
+    const float m = a.norm[2 * r], ls = a.norm[2 * r + 1], ref = against(m);
+    const int64_t t = a.g_logp ? (int64_t)((const ID*)a.targets)[r] : -1;
+    const float gl = t >= 0 && t < vocab ? a.g_logp[r] : 0.f;
+    const float ge = ENT ? a.g_entropy[r] : 0.f, h = ENT ? a.entropy[r] : 0.f;
+    const float scale = m == -INFINITY ? 0.f : a.scale;
+    auto grad = [&](float z, uint32_t j) {
+      const float ln = z * a.scale - ref - ls, p = __builtin_amdgcn_exp2f(ln * LOG2E);
+      float y = gl;
+      if (ENT) y = fmaf(ge, fmaxf(ln, -150.f) + h, gl);
+      return m == -INFINITY ? 0.f : ((j == t ? gl : 0.f) - p * y) * scale;
+    };
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const uint32_t j = j0 + i * 64 * V;
+      if (j + V <= vocab) {
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = grad(q[i].get(e), j + e);
+        q[i].put(y);
+        q[i].store(d + j);
+      } else {
+        for (uint32_t e = j; e < vocab; ++e) d[e] = from_float<T>(grad(to_float(x[e]), e));
+      }
     }
   }
 }
 
-template <class T, class ID>
-__global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a) {
-  const int64_t r = blockIdx.y;
-  for (int64_t row = r; row < a.rows; row += gridDim.y) {
-    const T* x = (const T*)a.logits + row * a.stride;
-    T* d = (T*)a.d + row * a.d_stride;
-    const float m = a.norm[2 * row], ls = a.norm[2 * row + 1], ref = m == -INFINITY ? 0.f : m;
-    const int64_t t = a.g_logp ? (int64_t)((const ID*)a.targets)[row] : -1;
-    const float gl = t >= 0 && t < a.vocab ? a.g_logp[row] : 0.f;
-    const float ge = a.g_entropy ? a.g_entropy[row] : 0.f, h = a.g_entropy ? a.entropy[row] : 0.f;
-    for (int64_t j = (int64_t)blockIdx.x * LB + threadIdx.x; j < a.vocab; j += (int64_t)gridDim.x * LB) {
-      const float ln = to_float(x[j]) * a.scale - ref - ls, p = expf(ln);
-      float y = (j == t ? gl : 0.f) - gl * p;
-      if (a.g_entropy) y -= ge * p * (fmaxf(ln, -150.f) + h);
-      d[j] = from_float<T>(m == -INFINITY ? 0.f : y * a.scale);
-    }
-  }
+// ------------------------------------------------------------------------------------------------------------ launches
+// A long row among few is dealt out in parts so that the chip has about 1024 workgroups, four to a compute unit, and a thread one
+// vector of its own at least.
+struct Split { int parts, part; };
+Split split(int64_t rows, int64_t vocab) {
+  if (vocab <= SHORT_ROW) return {1, (int)vocab};
+  const int64_t want = (1024 + rows - 1) / rows, grain = LB * 8, most = (vocab + grain - 1) / grain;
+  const int64_t parts = want < most ? want : most, part = ((vocab + parts - 1) / parts + grain - 1) / grain * grain;
+  return {(int)((vocab + part - 1) / part), (int)part};
 }
 
-int64_t logp_workspace(int64_t, int64_t, int) { return 0; }
+int64_t logp_workspace(int64_t rows, int64_t vocab, int top) {
+  if (rows == 0) return 0;
+  const Split s = split(rows, vocab);
+  return s.parts > 1 ? rows * s.parts * (int64_t)part_bytes(top) : 0;
+}
+
+template <class F> void with_flag(bool b, F&& f) { b ? f(std::true_type()) : f(std::false_type()); }
 
 void launch_logp(const LogpArgs& a, int dtype, int id_bits, hipStream_t s) {
-  with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) {
-    hipLaunchKernelGGL((k_logp<decltype(t), decltype(id)>), dim3((unsigned)a.rows), dim3(LB), 0, s, a);
-  }); });
+  const Split sp = split(a.rows, a.vocab);
+  with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) { with_flag(a.top > 0, [&](auto top) {
+    using T = decltype(t); using ID = decltype(id);
+    constexpr bool TOP = decltype(top)::value;
+    if (a.vocab <= SHORT_ROW) {
+      hipLaunchKernelGGL((k_logp<T, ID, TOP, true>), dim3((unsigned)((a.rows + WAVES - 1) / WAVES)), dim3(LB), 0, s, a, 1, (int)a.vocab);
+      return;
+    }
+    hipLaunchKernelGGL((k_logp<T, ID, TOP, false>), dim3((unsigned)(a.rows * sp.parts)), dim3(LB), 0, s, a, sp.parts, sp.part);
+    if (sp.parts > 1) hipLaunchKernelGGL((k_logp_join<T, ID, TOP>), dim3((unsigned)a.rows), dim3(LB), 0, s, a, sp.parts);
+  }); }); });
 }
 
 void launch_logp_grad(const LogpGradArgs& a, int dtype, int id_bits, hipStream_t s) {
-  const int64_t want = (a.vocab + 4 * LB - 1) / (4 * LB);
-  const dim3 grid((unsigned)(want < 256 ? want : 256), (unsigned)(a.rows < 32768 ? a.rows : 32768));
-  with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) {
-    hipLaunchKernelGGL((k_logp_grad<decltype(t), decltype(id)>), grid, dim3(LB), 0, s, a);
-  }); });
+  with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) { with_flag(a.g_entropy != nullptr, [&](auto ent) {
+    using T = decltype(t);
+    const int64_t piece = 64 * 4 * Sixteen<T>::V, per_row = (a.vocab + piece - 1) / piece, pieces = a.rows * per_row, groups = (pieces + WAVES - 1) / WAVES;
+    hipLaunchKernelGGL((k_logp_grad<T, decltype(id), decltype(ent)::value>), dim3((unsigned)(groups < (1 << 24) ? groups : 1 << 24)), dim3(LB), 0, s, a, pieces, (int)per_row);
+  }); }); });
 }
 
 }  // namespace pb

@@ -114,6 +114,7 @@ def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, w
     grad_scale: None or a float32 tensor of one element on the GPU that gradients are multiplied by.  predicted: None, or
     tensors that receive the weights as they will be after `horizon` more such steps (0: copies, in their own type)."""
     import torch
+    _DTYPE = torch.Tensor.dtype.__get__
     lib = _library()
     params, grads = list(params), list(grads)
     n = len(params)
@@ -125,24 +126,27 @@ def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, w
     for t, kind, what in ((step_dev, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale")):
         if t is not None and (t.dtype != kind or t.numel() != 1):
             raise PBError(f"adamw_step: {what} must be one element of {kind}")
-    index = _on_gpu("adamw_step", m, v, m_exp, v_exp, step_dev, grad_scale, *params, *grads, *hats)
-    _dense("adamw_step", m, v, m_exp, v_exp, *params, *grads, *hats)
-    sizes = [p.numel() for p in params]
-    for ts in (grads, hats):
-        if ts and [t.numel() for t in ts] != sizes:
-            raise PBError("adamw_step: gradients and predicted tensors must have their parameters' sizes")
+    T = torch.Tensor
+    every = params + grads + hats        # (hundreds of them: a call of each for all of them at once)
+    index = _on_gpu("adamw_step", m, v, m_exp, v_exp, step_dev, grad_scale)
+    if every and set(map(T.get_device, every)) != {index}:
+        raise PBError("adamw_step: all tensors must be on one GPU")
+    _dense("adamw_step", m, v, m_exp, v_exp)
+    if not all(map(T.is_contiguous, every)):
+        raise PBError("adamw_step: tensors must be contiguous")
+    sizes = list(map(T.numel, every))
+    if sizes != sizes[:n] * (len(every) // n if n else 0):
+        raise PBError("adamw_step: gradients and predicted tensors must have their parameters' sizes")
     for name, ts in (("w_type", params), ("g_type", grads), ("w_hat_type", hats)):
-        if len({t.dtype for t in ts}) > 1:
+        if len(set(map(_DTYPE, ts))) > 1:
             raise PBError("adamw_step: the tensors of a list must be of one type")
         if ts:
             setattr(d, name, _type(ts[0], "adamw_step: tensors"))
+    at = list(map(T.data_ptr, every))
     rec = np.zeros(n, dtype=_TENSOR)
-    rec["w"] = [p.data_ptr() for p in params]
-    rec["g"] = [g.data_ptr() for g in grads]
+    rec["w"], rec["g"], rec["n"], rec["weight_decay"] = at[:n], at[n:2 * n], sizes[:n], weight_decay
     if hats:
-        rec["w_hat"] = [h.data_ptr() for h in hats]
-    rec["n"] = sizes
-    rec["weight_decay"] = weight_decay
+        rec["w_hat"] = at[2 * n:]
     total = int((-(-rec["n"] // ADAMW_BLOCK) * ADAMW_BLOCK).sum())
     eight = m.dtype == torch.uint8
     if v.dtype != m.dtype or m.dtype not in (torch.uint8, torch.float32) or m.numel() != total or v.numel() != total:
