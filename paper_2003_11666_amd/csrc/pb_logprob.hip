@@ -84,26 +84,89 @@ __device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
 }
 
-// The best keys that a wavefront has seen, in falling order, one in each lane; a key enters if it beats the `top`-th.  Few do:
-// of n keys in no order about top * ln(n / top), each of which costs some twenty instructions.
+// Another lane's value: of lane ^ M.
+template <int M> __device__ __forceinline__ uint32_t of_lane_xor(uint32_t x) {
+  auto dpp = [](uint32_t v, auto C) { return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, decltype(C)::value, 0xF, 0xF, false); };
+  if constexpr (M == 1) return dpp(x, std::integral_constant<int, 0xB1>());         // quad_perm [1,0,3,2]
+  else if constexpr (M == 2) return dpp(x, std::integral_constant<int, 0x4E>());    // quad_perm [2,3,0,1]
+  else if constexpr (M == 4) return dpp(dpp(x, std::integral_constant<int, 0x141>()), std::integral_constant<int, 0x1B>());   // row_half_mirror (7), quad_perm (3)
+  else if constexpr (M == 8) return dpp(x, std::integral_constant<int, 0x128>());   // row_ror:8
+  else if constexpr (M == 16) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F);
+  else return (uint32_t)__shfl_xor((int)x, M, 64);
+}
+template <int M> __device__ __forceinline__ uint64_t of_lane_xor(uint64_t x) {
+  return (uint64_t)of_lane_xor<M>((uint32_t)(x >> 32)) << 32 | of_lane_xor<M>((uint32_t)x);
+}
+template <int M> __device__ __forceinline__ float of_lane_xor(float x) { return __uint_as_float(of_lane_xor<M>(__float_as_uint(x))); }
+// A step of a bitonic network: lanes M apart, the larger value to the lower lane where `falling`.
+template <int M, class T> __device__ __forceinline__ void order(T& x, bool falling) {
+  const T y = of_lane_xor<M>(x);
+  const bool low = (threadIdx.x & M) == 0;
+  x = (x > y) == (low == falling) ? x : y;
+}
+template <int M, class T> __device__ __forceinline__ void merge(T& x, bool falling) {   // of 2 M lanes that rise and then fall, or the other way
+  order<M>(x, falling);
+  if constexpr (M > 1) merge<M / 2>(x, falling);
+}
+template <int N = 64, class T> __device__ __forceinline__ void sort(T& x, bool falling = true) {   // of N lanes
+  if constexpr (N > 2) sort<N / 2>(x, (threadIdx.x & (N / 2)) == 0);
+  merge<N / 2>(x, falling);
+}
+
+// The best keys that a wavefront has seen, in falling order, one in each lane.  What may be among them is gathered in LDS, 64
+// at a time are sorted and merged with the list (some 200 instructions; one at a time would be 20 each, one behind the other).
+// The bar is the top-th of the list.
 struct Best {
   uint64_t key = 0, bar = 0;   // the lane's key; the top-th of all
   float bar_logit;             // a logit below it cannot enter (NaN: any can)
-  int top;
-  __device__ __forceinline__ Best(int top) : bar_logit(key_logit(0)), top(top) {}
+  int top, waiting = 0;
+  uint64_t* lds;               // 128 keys
+  __device__ __forceinline__ Best(int top, uint64_t* lds) : bar_logit(key_logit(0)), top(top), lds(lds) {}
+  __device__ __forceinline__ void raise() {
+    bar = lane_of(key, top - 1);
+    bar_logit = key_logit(bar);
+  }
+  // x: keys that rise from lane 0 on
+  __device__ __forceinline__ void merge_rising(uint64_t x) {
+    key = x > key ? x : key;
+    merge<32>(key, true);
+    raise();
+  }
+  __device__ __forceinline__ void sort_in(uint64_t x) {
+    sort(x, false);
+    merge_rising(x);
+  }
+  __device__ __forceinline__ void fence() {   // (LDS that other lanes of the wavefront wrote or will read)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
   __device__ __forceinline__ void enter(uint64_t k) {   // of every lane; 0 for none
     const int lane = threadIdx.x & 63;
-    for (uint64_t more = __ballot(k > bar); more; more &= __ballot(k > bar)) {
-      const int from = __builtin_ctzll(more);
-      const uint64_t x = lane_of(k, from);
-      const int place = __popcll(__ballot(key > x));
-      const uint64_t left = (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(key >> 32), 0x138, 0xF, 0xF, false) << 32 |
-                            (uint32_t)__builtin_amdgcn_update_dpp(0, (int)key, 0x138, 0xF, 0xF, false);   // of the lane before
-      key = lane < place ? key : lane == place ? x : left;
-      bar = lane_of(key, top - 1);
-      more &= ~(1ull << from);
-    }
-    bar_logit = key_logit(bar);
+    const uint64_t who = __ballot(k > bar);
+    if (who == 0) return;
+    if (k > bar) lds[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = k;
+    waiting += __popcll(who);
+    fence();
+    if (waiting < 64) return;
+    const uint64_t x = lds[lane], rest = lds[64 + lane];   // (the rest may be what never was written: then it is not counted)
+    fence();
+    lds[lane] = rest;
+    waiting -= 64;
+    fence();
+    sort_in(x);
+  }
+  __device__ __forceinline__ void finish() {
+    const int lane = threadIdx.x & 63;
+    if (waiting == 0) return;
+    const uint64_t x = lane < waiting ? lds[lane] : 0;
+    waiting = 0;
+    fence();
+    sort_in(x);
+  }
+  // x: the largest of each lane's logits, one of them; top of them at least are no worse than the top-th of these
+  __device__ __forceinline__ void start(float x) {
+    sort(x);
+    bar_logit = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), top - 1));
   }
 };
 
@@ -113,6 +176,7 @@ template <class T, bool TOP>
 __device__ __forceinline__ void scan(const T* x, uint32_t lo, uint32_t hi, uint32_t wave, uint32_t waves, float scale, Sums& a, Best& best) {
   constexpr uint32_t V = Sixteen<T>::V, U = 4;   // four requests of a lane under way
   const uint32_t lane = threadIdx.x & 63, whole = lo + (hi - lo) / V * V;
+  bool first = true;
   for (uint32_t j0 = lo + (wave * 64 + lane) * V; j0 - lane * V < whole; j0 += U * waves * 64 * V) {
     Sixteen<T> q[U];
 #pragma unroll
@@ -120,27 +184,33 @@ __device__ __forceinline__ void scan(const T* x, uint32_t lo, uint32_t hi, uint3
       const uint32_t j = j0 + i * waves * 64 * V;
       if (j < whole) q[i].load(x + j);
     }
+    float high = -INFINITY;
 #pragma unroll
     for (uint32_t i = 0; i < U; ++i) {
       const uint32_t j = j0 + i * waves * 64 * V;
       if (j - lane * V >= whole) break;
-      const bool mine = j < whole;
       float y[V];
-      bool high = false;
 #pragma unroll
       for (uint32_t e = 0; e < V; ++e) {
-        const float z = mine ? q[i].get(e) : -INFINITY;
-        if (TOP) high |= mine && !(z < best.bar_logit);
+        const float z = j < whole ? q[i].get(e) : -INFINITY;
+        if (TOP) high = fmaxf(high, z);
         y[e] = z * scale;
       }
       take(a, y);
-      if (TOP && __any(high)) {
+    }
+    if (!TOP) continue;
+    if (first) best.start(high);
+    first = false;
+    if (__all(high < best.bar_logit && a.s == a.s)) continue;   // (a NaN is above the bar, and in the sum)
 #pragma unroll
-        for (uint32_t e = 0; e < V; ++e) {
-          const float z = q[i].get(e);
-          const bool may = mine && !(z < best.bar_logit);
-          if (__any(may)) best.enter(may ? top_key(z, j + e) : 0);
-        }
+    for (uint32_t i = 0; i < U; ++i) {
+      const uint32_t j = j0 + i * waves * 64 * V;
+      if (j - lane * V >= whole) break;
+#pragma unroll
+      for (uint32_t e = 0; e < V; ++e) {
+        const float z = q[i].get(e);
+        const bool may = j < whole && !(z < best.bar_logit);
+        if (__any(may)) best.enter(may ? top_key(z, j + e) : 0);
       }
     }
   }
@@ -175,18 +245,21 @@ __device__ __forceinline__ void give(const LogpArgs& a, int64_t r, const Sums& w
 }
 
 // Of the workgroup's wavefronts into the first one.
-struct JoinLds { Sums w[WAVES]; uint64_t key[WAVES][64]; };
+struct JoinLds { Sums w[WAVES]; uint64_t key[WAVES][128]; };   // (keys: of a wavefront's own before the join)
 template <bool TOP> __device__ __forceinline__ void join_waves(Sums& a, Best& best, JoinLds& lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   join_lanes(a);
   if (lane == 0) lds.w[wave] = a;
-  if (TOP) lds.key[wave][lane] = best.key;
+  if (TOP) {
+    best.finish();
+    lds.key[wave][63 - lane] = best.key;
+  }
   __syncthreads();
   if (wave) return;
   a = lane < WAVES ? lds.w[lane] : NOTHING;
   join_lanes(a);
   if (TOP)
-    for (int i = 1; i < WAVES; ++i) best.enter(lane < best.top ? lds.key[i][lane] : 0);
+    for (int i = 1; i < WAVES; ++i) best.merge_rising(lds.key[i][lane]);
 }
 
 // What a workgroup that takes a part of a row leaves for the one that joins them: its sums, then its alternatives.
@@ -202,10 +275,11 @@ __global__ void __launch_bounds__(LB) k_logp(const LogpArgs a, int parts, int pa
   if (SHORT && r >= a.rows) return;
   const T* x = (const T*)a.logits + r * a.stride;
   Sums w = NOTHING;
-  Best best(a.top);
+  Best best(a.top, lds.key[wave]);
   if (SHORT) {
     scan<T, TOP>(x, 0, (uint32_t)a.vocab, 0, 1, a.scale, w, best);
     join_lanes(w);
+    if (TOP) best.finish();
     give<T, ID>(a, r, w, best);
     return;
   }
@@ -230,7 +304,7 @@ __global__ void __launch_bounds__(LB) k_logp_join(const LogpArgs a, int parts) {
   const size_t bytes = part_bytes(a.top);
   const char* at = (const char*)a.workspace + r * parts * bytes;
   Sums w = NOTHING;
-  Best best(a.top);
+  Best best(a.top, lds.key[wave]);
   for (int i = threadIdx.x; i < parts; i += LB) {
     Sums p = *(const Sums*)(at + i * bytes);
     const float m = fmaxf(w.m, p.m);
@@ -239,9 +313,19 @@ __global__ void __launch_bounds__(LB) k_logp_join(const LogpArgs a, int parts) {
     w.s += p.s;
     w.u += p.u;
   }
-  if (TOP)   // (a part's best first: the rest seldom enters)
-    for (int k = 0; k < a.top; ++k)
-      for (int i0 = wave * 64; i0 < parts; i0 += LB) best.enter(i0 + lane < parts ? ((const uint64_t*)(at + (i0 + lane) * bytes + 16))[k] : 0);
+  if (TOP) {   // (a part in each lane, or several of its keys in several; where no part's next one enters, no later one does)
+    int across = 64;
+    while (across / 2 >= parts) across /= 2;
+    for (int i0 = wave * 64; i0 < parts; i0 += LB) {
+      const int i = i0 + lane % across;
+      for (int k = lane / across; k - lane / across < a.top; k += 64 / across) {
+        const uint64_t x = i < parts && k < a.top ? ((const uint64_t*)(at + i * bytes + 16))[k] : 0;
+        if (!__any(x > best.bar)) break;
+        best.enter(x);
+      }
+      best.finish();
+    }
+  }
   join_waves<TOP>(w, best, lds);
   if (wave == 0) give<T, ID>(a, r, w, best);
 }
