@@ -4,111 +4,467 @@
 namespace pb {
 
 constexpr int EB = 256;   // threads per workgroup
+constexpr int EW = EB / 64;
 
+// V columns of a row as floats, from column j on, of which `have` exist.
+template <class T, int V> __device__ __forceinline__ void read_columns(float (&f)[V], const T* p, int have) {
+  if (have >= V) {
+#pragma unroll
+    for (int i = 0; i < V; i += Sixteen<T>::V) {
+      Sixteen<T> q;
+      q.load(p + i);
+#pragma unroll
+      for (int e = 0; e < Sixteen<T>::V; ++e) f[i + e] = q.get(e);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = e < have ? to_float(p[e]) : 0.f;
+  }
+}
+template <class T, int V> __device__ __forceinline__ void write_columns(T* p, const float (&f)[V], int have) {
+  if (have >= V) {
+#pragma unroll
+    for (int i = 0; i < V; i += Sixteen<T>::V) {
+      Sixteen<T> q;
+      float part[Sixteen<T>::V];
+#pragma unroll
+      for (int e = 0; e < Sixteen<T>::V; ++e) part[e] = f[i + e];
+      q.put(part);
+      q.store(p + i);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < have) p[e] = from_float<T>(f[e]);
+  }
+}
+
+constexpr int EV = 8;              // columns of a lane: 16 bytes of bf16
+constexpr int SLICE = 64 * EV;     // of a wavefront
+
+// ------------------------------------------------------------------------------------------------------------- lookup
+// Bound by memory.  A wavefront takes SLICE columns of one token.
 template <class T, class O, class ID>
-__global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a) {
-  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
-    const int64_t id = ((const ID*)a.ids)[i];
-    const bool there = id >= 0 && id < a.vocab;
-    const T* row = (const T*)a.table + (there ? id : 0) * a.dim;
-    O* out = (O*)a.out + i * a.dim;
-    for (int64_t j = threadIdx.x; j < a.dim; j += EB) out[j] = from_float<O>(there ? to_float(row[j]) * a.scale : 0.f);
+__global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a, int64_t pieces, int slices) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces; p += (int64_t)gridDim.x * EW) {
+    const int64_t i = p / slices, j = (p - i * slices) * SLICE + lane * EV, id = ((const ID*)a.ids)[i];
+    const int64_t have = a.dim - j;
+    if (have <= 0) continue;
+    float f[EV] = {};
+    if (id >= 0 && id < a.vocab) read_columns<T, EV>(f, (const T*)a.table + id * a.dim + j, have < EV ? (int)have : EV);
+#pragma unroll
+    for (int e = 0; e < EV; ++e) f[e] *= a.scale;
+    if (!(id >= 0 && id < a.vocab)) {
+#pragma unroll
+      for (int e = 0; e < EV; ++e) f[e] = 0.f;
+    }
+    write_columns<O, EV>((O*)a.out + i * a.dim + j, f, have < EV ? (int)have : EV);
   }
 }
 
-// ---- gradient: the places of the tokens sorted by id, equal ids in the order of their places, then the sum of each id's rows
-__global__ void __launch_bounds__(EB) k_zero(uint32_t* p, int64_t n) {
-  for (int64_t i = (int64_t)blockIdx.x * EB + threadIdx.x; i < n; i += (int64_t)gridDim.x * EB) p[i] = 0;
-}
+// --------------------------------------------------------------------------------------------- sorting tokens by their ids
+// Stable, by digits of the id from the lowest up; an id outside the table becomes `vocab`, behind all others.  Digits are as
+// wide as the fewest passes make them, 9 bits at most: two passes for up to 2^18 ids.
+constexpr int DIGIT = 9, BINS = 1 << DIGIT;
+constexpr int ONE_WG = 8192;        // up to so many tokens one workgroup sorts in LDS
+constexpr int TILE = 4096;          // tokens per workgroup of a pass over more
+template <class ID> __device__ __forceinline__ uint32_t id_key(ID id, int64_t vocab) { return (uint32_t)(id >= 0 && (int64_t)id < vocab ? (int64_t)id : vocab); }
 
-template <class ID>
-__global__ void __launch_bounds__(EB) k_count(const ID* ids, int64_t n, int64_t vocab, uint32_t* count) {
-  for (int64_t i = (int64_t)blockIdx.x * EB + threadIdx.x; i < n; i += (int64_t)gridDim.x * EB) {
-    const int64_t id = ids[i];
-    if (id >= 0 && id < vocab) atomicAdd(count + id, 1u);
+// Places of 64 tokens among those of equal digits that the wavefront has met: count holds these, one for each digit.
+__device__ __forceinline__ uint32_t place_in_wave(uint32_t d, bool mine, int width, volatile uint32_t* count) {
+  uint64_t same = __ballot(mine);
+  for (int b = 0; b < width; ++b) {
+    const bool one = d >> b & 1;
+    const uint64_t w = __ballot(one);
+    same &= one ? w : ~w;
   }
-}
-
-// count -> the first place of each id among the sorted ones, one workgroup
-__global__ void __launch_bounds__(EB) k_starts(uint32_t* count, int64_t vocab) {
-  __shared__ uint32_t part[EB];
-  const int64_t per = (vocab + EB - 1) / EB, lo = per * threadIdx.x, hi = lo + per < vocab ? lo + per : vocab;
-  uint32_t s = 0;
-  for (int64_t i = lo; i < hi; ++i) s += count[i];
-  part[threadIdx.x] = s;
-  __syncthreads();
+  const int lane = threadIdx.x & 63, before = __popcll(same & ((1ull << lane) - 1));
   uint32_t at = 0;
-  for (int i = 0; i < (int)threadIdx.x; ++i) at += part[i];
-  for (int64_t i = lo; i < hi; ++i) {
-    const uint32_t c = count[i];
-    count[i] = at;
-    at += c;
+  if (mine) at = count[d];
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (mine && before == 0) count[d] = at + (uint32_t)__popcll(same);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  return at + (uint32_t)before;
+}
+
+// Exclusive sum over the threads of a workgroup, WAVES wavefronts.
+template <int WAVES> __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t s = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t y = (uint32_t)__shfl_up((int)s, o, 64);
+    if (lane >= o) s += y;
+  }
+  if (lane == 63) lds[wave] = s;
+  __syncthreads();
+  uint32_t base = 0;
+  for (int i = 0; i < wave; ++i) base += lds[i];
+  __syncthreads();
+  return base + s - x;
+}
+
+constexpr int SW = 16;              // wavefronts of the workgroup that sorts alone
+template <class ID>
+__global__ void __launch_bounds__(64 * SW) k_sort(const ID* ids, int n, int64_t vocab, int width, int passes, uint32_t* key_out, uint32_t* place_out) {
+  __shared__ uint32_t key[ONE_WG], place[ONE_WG], count[SW][BINS], part[SW];
+  constexpr int G = ONE_WG / (64 * SW);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+  const int per = (n + 64 * SW - 1) / (64 * SW);   // groups of 64 for each wavefront
+  uint32_t k[G], p[G], r[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int i = (wave * per + g) * 64 + lane;
+    k[g] = g < per && i < n ? id_key(ids[i], vocab) : 0;
+    p[g] = (uint32_t)i;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    for (int i = tid; i < SW * BINS; i += 64 * SW) (&count[0][0])[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const bool mine = g < per && (wave * per + g) * 64 + lane < n;
+      if (g < per) r[g] = place_in_wave(k[g] >> pass * width & ((1u << width) - 1), mine, width, count[wave]);
+    }
+    __syncthreads();
+    // the first place of each digit's tokens of each wavefront: two threads to a digit, eight wavefronts each
+    static_assert(BINS * 2 == 64 * SW, "two threads to a digit");
+    uint32_t c[SW / 2], s = 0;
+#pragma unroll
+    for (int w = 0; w < SW / 2; ++w) {
+      c[w] = count[(tid & 1) * (SW / 2) + w][tid >> 1];
+      s += c[w];
+    }
+    uint32_t at = sum_before<SW>(s, part);
+#pragma unroll
+    for (int w = 0; w < SW / 2; ++w) {
+      count[(tid & 1) * (SW / 2) + w][tid >> 1] = at;
+      at += c[w];
+    }
+    __syncthreads();
+    const bool last = pass + 1 == passes;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (!(g < per && (wave * per + g) * 64 + lane < n)) continue;
+      const uint32_t to = count[wave][k[g] >> pass * width & ((1u << width) - 1)] + r[g];
+      (last ? key_out : key)[to] = k[g];
+      (last ? place_out : place)[to] = p[g];
+    }
+    __syncthreads();
+    if (last) break;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int i = (wave * per + g) * 64 + lane;
+      if (!(g < per && i < n)) continue;
+      k[g] = key[i];
+      p[g] = place[i];
+    }
+    // (the next pass writes key and place only behind barriers)
   }
 }
 
-// one workgroup takes the tokens in order, EB at a time; count[id] moves from the first place of the id to the one behind its last
-template <class ID>
-__global__ void __launch_bounds__(EB) k_place(const ID* ids, int64_t n, int64_t vocab, uint32_t* count, uint32_t* order) {
-  __shared__ int64_t now[EB];
-  for (int64_t base = 0; base < n; base += EB) {
-    const int64_t i = base + threadIdx.x;
-    int64_t id = i < n ? (int64_t)ids[i] : -1;
-    if (id >= vocab) id = -1;
-    now[threadIdx.x] = id;
+// One pass over more tokens, in tiles: how often each digit occurs in each tile ...
+template <class ID, bool FIRST>
+__device__ __forceinline__ uint32_t key_at(const void* in, int64_t i, int64_t vocab) { return FIRST ? id_key(((const ID*)in)[i], vocab) : ((const uint32_t*)in)[i]; }
+
+template <class ID, bool FIRST>
+__global__ void __launch_bounds__(EB) k_digits(const void* in, int64_t n, int64_t vocab, int shift, int width, int64_t tiles, uint32_t* counts) {
+  __shared__ uint32_t count[BINS];
+  for (int i = threadIdx.x; i < BINS; i += EB) count[i] = 0;
+  __syncthreads();
+  const int64_t i0 = (int64_t)blockIdx.x * TILE;
+#pragma unroll
+  for (int g = 0; g < TILE / EB; ++g) {
+    const int64_t i = i0 + g * EB + threadIdx.x;
+    if (i < n) atomicAdd(&count[key_at<ID, FIRST>(in, i, vocab) >> shift & ((1u << width) - 1)], 1u);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 1 << width; i += EB) counts[i * tiles + blockIdx.x] = count[i];
+}
+
+// ... the sums over the tiles before, a workgroup to a digit ...
+__global__ void __launch_bounds__(EB) k_tiles(uint32_t* counts, int64_t tiles, uint32_t* total) {
+  __shared__ uint32_t part[EW], carry;
+  uint32_t* c = counts + (int64_t)blockIdx.x * tiles;
+  uint32_t base = 0;
+  for (int64_t i0 = 0; i0 < tiles; i0 += EB) {
+    const int64_t i = i0 + threadIdx.x;
+    const uint32_t x = i < tiles ? c[i] : 0, at = base + sum_before<EW>(x, part);
+    if (i < tiles) c[i] = at;
+    if (threadIdx.x == EB - 1) carry = at + x;
     __syncthreads();
-    uint32_t before = 0, behind = 0;
-    for (int j = 0; j < EB; ++j) {
-      if (now[j] != id) continue;
-      before += j < (int)threadIdx.x;
-      behind += j > (int)threadIdx.x;
+    base = carry;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) total[blockIdx.x] = base;
+}
+
+// ... and each token to its place.
+template <class ID, bool FIRST>
+__global__ void __launch_bounds__(EB)
+k_scatter(const void* in, const uint32_t* place_in, int64_t n, int64_t vocab, int shift, int width, int64_t tiles, const uint32_t* counts, const uint32_t* total,
+          uint32_t* key_out, uint32_t* place_out) {
+  __shared__ uint32_t count[EW][BINS], part[EW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+  constexpr int G = TILE / EB;
+  for (int i = tid; i < EW * BINS; i += EB) (&count[0][0])[i] = 0;
+  const int64_t i0 = (int64_t)blockIdx.x * TILE + wave * (TILE / EW) + lane;
+  const uint32_t mask = (1u << width) - 1;
+  uint32_t k[G], p[G], r[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int64_t i = i0 + g * 64;
+    k[g] = i < n ? key_at<ID, FIRST>(in, i, vocab) : 0;
+    p[g] = FIRST || i >= n ? (uint32_t)i : place_in[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < G; ++g) r[g] = place_in_wave(k[g] >> shift & mask, i0 + g * 64 < n, width, count[wave]);
+  __syncthreads();
+  // the first place of each digit's tokens of each wavefront: two digits to a thread
+  static_assert(BINS == 2 * EB, "two digits to a thread");
+  uint32_t t[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) t[h] = 2 * tid + h <= (int)mask ? total[2 * tid + h] : 0;
+  uint32_t at = sum_before<EW>(t[0] + t[1], part);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int d = 2 * tid + h;
+    uint32_t a = at + (d <= (int)mask ? counts[d * tiles + blockIdx.x] : 0);
+    at += t[h];
+#pragma unroll
+    for (int w = 0; w < EW; ++w) {
+      const uint32_t c = count[w][d];
+      count[w][d] = a;
+      a += c;
     }
-    uint32_t at = 0;
-    if (id >= 0) {
-      at = __hip_atomic_load(count + id, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + before;
-      order[at] = (uint32_t)i;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    if (i0 + g * 64 >= n) continue;
+    const uint32_t to = count[wave][k[g] >> shift & mask] + r[g];
+    key_out[to] = k[g];
+    place_out[to] = p[g];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------- the sums
+// The sorted tokens are dealt out in chunks, SLICE columns of a chunk to a wavefront, which adds up its rows as they come.  The
+// sum of an id whose tokens all lie in the chunk is final.  Of an id that goes on beyond it the chunk leaves a part: one of the
+// id that was there before its first token, one of the id that starts in it and goes on; k_join adds up the parts.  So
+// the work does not depend on how often an id occurs, and the order of the sums on nothing but the tokens.  Bound by memory:
+// each row of gradients is read once, in whole cache lines.
+struct Sorted { const uint32_t *key, *place; int64_t n; int chunk; float* part; };   // part [chunk][2][dim]
+
+template <class O>
+__device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t id, int64_t j, float (&s)[EV], int have) {
+  O* out = (O*)a.d_table + id * a.dim + j;
+#pragma unroll
+  for (int e = 0; e < EV; ++e) s[e] *= a.scale;
+  if (a.add) {
+    float f[EV];
+    read_columns<O, EV>(f, out, have);
+#pragma unroll
+    for (int e = 0; e < EV; ++e) s[e] += f[e];
+  }
+  write_columns<O, EV>(out, s, have);
+}
+
+template <class T, class O>
+__device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& s, int64_t c, int64_t j) {
+  constexpr int B = 8;   // rows under way
+  const int lane = threadIdx.x & 63;
+  const int have = a.dim - j >= EV ? EV : a.dim > j ? (int)(a.dim - j) : 0;
+  const int64_t lo = c * s.chunk, hi = lo + s.chunk < s.n ? lo + s.chunk : s.n;
+  bool began_before = lo > 0 && s.key[lo - 1] == s.key[lo];
+  float acc[EV] = {};
+  auto part = [&](int which) {
+    write_columns<float, EV>(s.part + (2 * c + which) * a.dim + j, acc, have);
+#pragma unroll
+    for (int e = 0; e < EV; ++e) acc[e] = 0.f;
+  };
+  for (int64_t k0 = lo; k0 < hi; k0 += 64) {
+    const int64_t k = k0 + lane;
+    const uint32_t key = k < hi ? s.key[k] : (uint32_t)a.vocab, place = k < hi ? s.place[k] : 0;
+    const uint32_t next = k + 1 < s.n ? s.key[k + 1] : 0xFFFFFFFFu;
+    for (int b0 = 0; b0 < 64; b0 += B) {
+      float row[B][EV];
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)key, b0 + b), at = (uint32_t)__builtin_amdgcn_readlane((int)place, b0 + b);
+        if (id < (uint64_t)a.vocab) read_columns<T, EV>(row[b], (const T*)a.d_out + (int64_t)at * a.dim + j, have);
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)key, b0 + b);
+        if (id >= (uint64_t)a.vocab) return;   // the end of the chunk, or of the tokens that count
+#pragma unroll
+        for (int e = 0; e < EV; ++e) acc[e] += row[b][e];
+        const bool ends = (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id;
+        if (!ends && k0 + b0 + b + 1 < hi) continue;
+        if (ends && !began_before) {
+          put_row<O>(a, id, j, acc, have);
+#pragma unroll
+          for (int e = 0; e < EV; ++e) acc[e] = 0.f;
+        } else {
+          part(began_before ? 0 : 1);
+        }
+        began_before = false;
+      }
     }
-    __syncthreads();
-    if (id >= 0 && behind == 0) __hip_atomic_store(count + id, at + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
+  }
+}
+
+// Rows of the table that no token names, 64 to a wavefront: each lane looks its own up among the sorted ids.
+constexpr int EMPTY_ROWS = 64;
+template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArgs& a, const Sorted& s, int64_t r0) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = r0 + lane;
+  int64_t lo = 0, hi = s.n;   // the first sorted token of an id >= r
+  while (__any(lo < hi)) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (lo < hi) {
+      if ((int64_t)s.key[mid] < r) lo = mid + 1;
+      else hi = mid;
+    }
+  }
+  const bool empty = r < a.vocab && !(lo < s.n && (int64_t)s.key[lo] == r);
+  const float zero[EV] = {};
+  for (uint64_t more = __ballot(empty); more; more &= more - 1) {
+    O* out = (O*)a.d_table + (r0 + __builtin_ctzll(more)) * a.dim;
+    for (int64_t j = lane * EV; j < a.dim; j += SLICE) write_columns<O, EV>(out + j, zero, a.dim - j < EV ? (int)(a.dim - j) : EV);
   }
 }
 
 template <class T, class O>
-__global__ void __launch_bounds__(EB) k_sum(const EmbedGradArgs a, const uint32_t* behind, const uint32_t* order) {
-  for (int64_t v = blockIdx.x; v < a.vocab; v += gridDim.x) {
-    const uint32_t lo = v ? behind[v - 1] : 0, hi = behind[v];
-    if (lo == hi && a.add) continue;
-    O* out = (O*)a.d_table + v * a.dim;
-    for (int64_t j = threadIdx.x; j < a.dim; j += EB) {
-      float s = 0.f;
-      for (uint32_t k = lo; k < hi; ++k) s += to_float(((const T*)a.d_out)[(int64_t)order[k] * a.dim + j]);
-      s *= a.scale;
-      out[j] = from_float<O>(a.add ? to_float(out[j]) + s : s);
-    }
+__global__ void __launch_bounds__(EB) k_sums(const EmbedGradArgs a, const Sorted s, int64_t pieces, int slices, int64_t clears) {
+  for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces + clears; p += (int64_t)gridDim.x * EW) {
+    if (p >= pieces) clear_rows<O>(a, s, (p - pieces) * EMPTY_ROWS);
+    else sum_chunk<T, O>(a, s, p / slices, (p % slices) * SLICE + (threadIdx.x & 63) * EV);
   }
 }
 
+// The id that starts in a chunk and goes on beyond it: its part of the chunk and those of the chunks behind, dealt out to the
+// wavefronts of a workgroup.
+template <class O>
+__global__ void __launch_bounds__(EB) k_join(const EmbedGradArgs a, const Sorted s, int64_t chunks) {
+  __shared__ float sums[EW][SLICE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = blockIdx.x, lo = c * s.chunk, hi = lo + s.chunk;
+  if (hi >= s.n) return;
+  const uint32_t id = s.key[hi - 1];
+  if (id >= (uint64_t)a.vocab || s.key[hi] != id || (s.key[lo] == id && lo > 0 && s.key[lo - 1] == id)) return;
+  int64_t behind = 0;   // chunks behind this one that go on with the id
+  for (;;) {
+    const int64_t at = (c + 1 + behind + lane) * s.chunk;
+    const uint64_t on = __ballot(at < s.n && s.key[at < s.n ? at : 0] == id);
+    behind += on == ~0ull ? 64 : __builtin_ctzll(~on);
+    if (on != ~0ull) break;
+  }
+  for (int64_t j0 = (int64_t)blockIdx.y * SLICE; j0 < a.dim; j0 += (int64_t)gridDim.y * SLICE) {
+    const int64_t j = j0 + lane * EV;
+    const int have = a.dim - j >= EV ? EV : a.dim > j ? (int)(a.dim - j) : 0;
+    float acc[EV] = {};
+#pragma unroll 4
+    for (int64_t k = wave; k <= behind; k += EW) {
+      float f[EV];
+      read_columns<float, EV>(f, s.part + (2 * (c + k) + (k == 0)) * a.dim + j, have);
+#pragma unroll
+      for (int e = 0; e < EV; ++e) acc[e] += f[e];
+    }
+#pragma unroll
+    for (int e = 0; e < EV; ++e) sums[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (wave == 0) {
+      for (int w = 1; w < EW; ++w)
+#pragma unroll
+        for (int e = 0; e < EV; ++e) acc[e] += sums[w][e * 64 + lane];
+      put_row<O>(a, id, j, acc, have);
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ launches
+namespace {
+
+dim3 groups_for(int64_t wavefronts) {
+  const int64_t g = (wavefronts + EW - 1) / EW;
+  return dim3((unsigned)(g < (1 << 20) ? g : 1 << 20));
+}
+
+int64_t in_slices(int64_t dim) { return (dim + SLICE - 1) / SLICE; }
+
+// Tokens per chunk: 2048 chunks at most, so that few parts are left of an id that most tokens share, and 8 tokens at least.
+int chunk_of(int64_t n) { return (int)(n / 2048 < 8 ? 8 : (n + 2047) / 2048); }
+
+struct Layout { int64_t key[2], place[2], counts, total, part, bytes, tiles; };
+Layout layout(int64_t n, int64_t dim) {
+  Layout l = {};
+  auto take = [&](int64_t bytes) { const int64_t at = l.bytes; l.bytes += (bytes + 255) / 256 * 256; return at; };
+  const bool big = n > ONE_WG;
+  l.tiles = (n + TILE - 1) / TILE;
+  for (int i = 0; i < (big ? 2 : 1); ++i) {
+    l.key[i] = take(4 * n);
+    l.place[i] = take(4 * n);
+  }
+  if (big) {
+    l.counts = take(4 * BINS * l.tiles);
+    l.total = take(4 * BINS);
+  }
+  const int64_t chunk = chunk_of(n), chunks = (n + chunk - 1) / chunk;
+  l.part = take(8 * chunks * dim);
+  return l;
+}
+
+}  // namespace
+
 void launch_embed(const EmbedArgs& a, int dtype, int out_dtype, int id_bits, hipStream_t s) {
-  const unsigned grid = (unsigned)(a.n < (1 << 20) ? a.n : 1 << 20);
+  const int64_t slices = in_slices(a.dim), pieces = a.n * slices;
   with_type(dtype, [&](auto t) { with_type(out_dtype, [&](auto o) { with_id(id_bits, [&](auto id) {
-    hipLaunchKernelGGL((k_embed<decltype(t), decltype(o), decltype(id)>), dim3(grid), dim3(EB), 0, s, a);
+    hipLaunchKernelGGL((k_embed<decltype(t), decltype(o), decltype(id)>), groups_for(pieces), dim3(EB), 0, s, a, pieces, (int)slices);
   }); }); });
 }
 
-int64_t embed_grad_workspace(int64_t n, int64_t vocab, int64_t) { return 4 * (n + vocab); }
+int64_t embed_grad_workspace(int64_t n, int64_t, int64_t dim) { return n > 0 ? layout(n, dim).bytes : 0; }
 
 void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int id_bits, hipStream_t s) {
-  uint32_t *count = (uint32_t*)a.workspace, *order = count + a.vocab;
-  auto grid = [](int64_t n, int64_t most) { const int64_t g = (n + EB - 1) / EB; return dim3((unsigned)(g < most ? g : most)); };
-  hipLaunchKernelGGL(k_zero, grid(a.vocab, 4096), dim3(EB), 0, s, count, a.vocab);
+  char* ws = (char*)a.workspace;
+  const Layout l = layout(a.n, a.dim);
+  auto at = [&](int64_t o) { return (uint32_t*)(ws + o); };
+  int bits = 0;
+  while (a.vocab >> bits) ++bits;
+  const int passes = (bits + DIGIT - 1) / DIGIT, width = (bits + passes - 1) / passes;
+  int from = 0;
   if (a.n > 0) with_id(id_bits, [&](auto id) {
     using ID = decltype(id);
-    hipLaunchKernelGGL((k_count<ID>), grid(a.n, 4096), dim3(EB), 0, s, (const ID*)a.ids, a.n, a.vocab, count);
-    hipLaunchKernelGGL(k_starts, dim3(1), dim3(EB), 0, s, count, a.vocab);
-    hipLaunchKernelGGL((k_place<ID>), dim3(1), dim3(EB), 0, s, (const ID*)a.ids, a.n, a.vocab, count, order);
+    if (a.n <= ONE_WG) {
+      hipLaunchKernelGGL((k_sort<ID>), dim3(1), dim3(64 * SW), 0, s, (const ID*)a.ids, (int)a.n, a.vocab, width, passes, at(l.key[0]), at(l.place[0]));
+      return;
+    }
+    const dim3 grid((unsigned)l.tiles);
+    for (int p = 0; p < passes; ++p, from ^= 1) {
+      uint32_t *key = at(l.key[from]), *place = at(l.place[from]), *key_to = at(l.key[from ^ 1]), *place_to = at(l.place[from ^ 1]);
+      if (p == 0) hipLaunchKernelGGL((k_digits<ID, true>), grid, dim3(EB), 0, s, a.ids, a.n, a.vocab, 0, width, l.tiles, at(l.counts));
+      else hipLaunchKernelGGL((k_digits<ID, false>), grid, dim3(EB), 0, s, key, a.n, a.vocab, p * width, width, l.tiles, at(l.counts));
+      hipLaunchKernelGGL(k_tiles, dim3(1u << width), dim3(EB), 0, s, at(l.counts), l.tiles, at(l.total));
+      if (p == 0)
+        hipLaunchKernelGGL((k_scatter<ID, true>), grid, dim3(EB), 0, s, a.ids, nullptr, a.n, a.vocab, 0, width, l.tiles, at(l.counts), at(l.total), key_to, place_to);
+      else
+        hipLaunchKernelGGL((k_scatter<ID, false>), grid, dim3(EB), 0, s, key, place, a.n, a.vocab, p * width, width, l.tiles, at(l.counts), at(l.total), key_to, place_to);
+    }
   });
+  const int chunk = chunk_of(a.n);
+  const int64_t chunks = (a.n + chunk - 1) / chunk, slices = in_slices(a.dim), clears = a.add ? 0 : (a.vocab + EMPTY_ROWS - 1) / EMPTY_ROWS;
+  const Sorted sorted = {at(l.key[from]), at(l.place[from]), a.n, chunk, (float*)at(l.part)};
   with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) {
-    hipLaunchKernelGGL((k_sum<decltype(t), decltype(o)>), dim3((unsigned)(a.vocab < (1 << 20) ? a.vocab : 1 << 20)), dim3(EB), 0, s, a, count, order);
+    hipLaunchKernelGGL((k_sums<decltype(t), decltype(o)>), groups_for(chunks * slices + clears), dim3(EB), 0, s, a, sorted, chunks * slices, (int)slices, clears);
+    if (chunks > 1)
+      hipLaunchKernelGGL((k_join<decltype(o)>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(EB), 0, s, a, sorted, chunks);
   }); });
 }
 

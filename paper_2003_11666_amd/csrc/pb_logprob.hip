@@ -13,26 +13,6 @@ constexpr int WAVES = LB / 64;
 constexpr int64_t SHORT_ROW = 2048; // rows up to here are a wavefront's each
 constexpr float LOG2E = 1.44269504088896340736f;
 
-// 16 bytes of logits, on a boundary of one logit: rows start anywhere.
-template <class T> struct Sixteen {
-  typedef uint32_t words __attribute__((ext_vector_type(4)));
-  typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
-  static constexpr int V = 16 / sizeof(T);
-  words q;
-  __device__ __forceinline__ void load(const T* p) { q = __builtin_nontemporal_load((const loose*)p); }
-  __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store((loose)q, (loose*)p); }
-  __device__ __forceinline__ float get(int e) const {
-    const uint32_t w = q[e * sizeof(T) / 4];
-    return __uint_as_float(sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
-  }
-  __device__ __forceinline__ void put(const float (&f)[V]) {
-    struct alignas(16) { T x[V]; } k;
-#pragma unroll
-    for (int e = 0; e < V; ++e) k.x[e] = from_float<T>(f[e]);
-    q = __builtin_bit_cast(words, k);
-  }
-};
-
 // ------------------------------------------------------------------------------------------------------- running sums
 // Of the logits seen so far: maximum m, s = sum e^(x - m), u = sum (x - m) e^(x - m), passed over once.  -inf as maximum stands
 // for none that counts; a NaN, or +inf, makes s NaN.  (x - m is held above -150 in u, whose term is 0 from there on: 0 * -inf.)

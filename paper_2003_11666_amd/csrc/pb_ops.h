@@ -129,6 +129,26 @@ template <class T, int V> struct Vec {
   }
 };
 
+// 16 bytes of values on a boundary of one of them: rows of odd lengths start anywhere.
+template <class T> struct Sixteen {
+  typedef uint32_t words __attribute__((ext_vector_type(4)));
+  typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
+  static constexpr int V = 16 / sizeof(T);
+  words q;
+  __device__ __forceinline__ void load(const T* p) { q = __builtin_nontemporal_load((const loose*)p); }
+  __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store((loose)q, (loose*)p); }
+  __device__ __forceinline__ float get(int e) const {
+    const uint32_t w = q[e * sizeof(T) / 4];
+    return __uint_as_float(sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
+  }
+  __device__ __forceinline__ void put(const float (&f)[V]) {
+    struct alignas(16) { T x[V]; } k;
+#pragma unroll
+    for (int e = 0; e < V; ++e) k.x[e] = from_float<T>(f[e]);
+    q = __builtin_bit_cast(words, k);
+  }
+};
+
 // f(T{}, U{}) with the C++ types of two pb_dtype
 template <class F> void with_type(int t, F&& f) { t == PB_BF16 ? f(bf16()) : f(float()); }
 template <class F> void with_id(int bits, F&& f) { bits == 64 ? f(int64_t()) : f(int32_t()); }
