@@ -1,6 +1,4 @@
 // AdamW over many tensors at once, moments in 32 or in 8 bits (pb_adamw_step, pb_adamw_moments).
-#include <type_traits>
-
 #include "pb_ops.h"
 
 namespace pb {

@@ -67,27 +67,37 @@ __global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a, int64_t pieces,
 // Stable, by digits of the id from the lowest up; an id outside the table becomes `vocab`, behind all others.  Digits are as
 // wide as the fewest passes make them, 9 bits at most: two passes for up to 2^18 ids.
 constexpr int DIGIT = 9, BINS = 1 << DIGIT;
-constexpr int ONE_WG = 8192;        // up to so many tokens one workgroup sorts in LDS
-constexpr int TILE = 4096;          // tokens per workgroup of a pass over more
+constexpr int FEW = 16384;          // up to so many tokens are ranked by comparisons
+constexpr int TILE = 1024;          // tokens per workgroup of a pass over more
 template <class ID> __device__ __forceinline__ uint32_t id_key(ID id, int64_t vocab) { return (uint32_t)(id >= 0 && (int64_t)id < vocab ? (int64_t)id : vocab); }
 
-// Places of 64 tokens among those of equal digits that the wavefront has met: count holds these, one for each digit.
-__device__ __forceinline__ uint32_t place_in_wave(uint32_t d, bool mine, int width, volatile uint32_t* count) {
-  uint64_t same = __ballot(mine);
-  for (int b = 0; b < width; ++b) {
-    const bool one = d >> b & 1;
-    const uint64_t w = __ballot(one);
-    same &= one ? w : ~w;
+// Places of G groups of 64 tokens, one group after the other, among those of equal digits that the wavefront has met.  count
+// holds these, one for each digit, for this wavefront alone: the first lane of each digit adds its group's, and a
+// wavefront's LDS operations are done in their order, so that no group waits for the one before.
+template <int G> __device__ __forceinline__ void places_in_wave(const uint32_t (&digit)[G], const bool (&mine)[G], uint32_t* count, uint32_t (&place)[G]) {
+  const int lane = threadIdx.x & 63;
+  uint64_t same[G];
+  uint32_t at[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    same[g] = __ballot(mine[g]);
+#pragma unroll
+    for (int b = 0; b < DIGIT; ++b) {
+      const bool one = digit[g] >> b & 1;
+      const uint64_t w = __ballot(one);
+      same[g] &= one ? w : ~w;
+    }
   }
-  const int lane = threadIdx.x & 63, before = __popcll(same & ((1ull << lane) - 1));
-  uint32_t at = 0;
-  if (mine) at = count[d];
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  if (mine && before == 0) count[d] = at + (uint32_t)__popcll(same);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  return at + (uint32_t)before;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    at[g] = 0;
+    if (mine[g] && (same[g] & ((1ull << lane) - 1)) == 0) at[g] = atomicAdd(count + digit[g], (uint32_t)__popcll(same[g]));
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const uint32_t first = (uint32_t)__shfl((int)at[g], mine[g] ? __builtin_ctzll(same[g]) : 0, 64);
+    place[g] = first + (uint32_t)__popcll(same[g] & ((1ull << lane) - 1));
+  }
 }
 
 // Exclusive sum over the threads of a workgroup, WAVES wavefronts.
@@ -107,62 +117,64 @@ template <int WAVES> __device__ __forceinline__ uint32_t sum_before(uint32_t x, 
   return base + s - x;
 }
 
-constexpr int SW = 16;              // wavefronts of the workgroup that sorts alone
+// Few tokens: the place of one is how many come before it, each counted against all others.  A workgroup holds the ids of all
+// tokens in LDS, dealt out to 128 parts of its threads, and takes 32 tokens, four to a lane in each part: two instructions
+// for 64 comparisons and an LDS read for sixteen times as many (with one token to a lane these reads were the bound).  The 67
+// million comparisons of 8192 tokens take the chip 3.4 us; a radix sort in one workgroup took 31 us, one in tiles takes six
+// launches.
+constexpr int RANKED = 32, PER_LANE = 4, RB = 1024, PARTS = RB * PER_LANE / RANKED, PART = FEW / PARTS + 4;   // (4 words on: other banks)
 template <class ID>
-__global__ void __launch_bounds__(64 * SW) k_sort(const ID* ids, int n, int64_t vocab, int width, int passes, uint32_t* key_out, uint32_t* place_out) {
-  __shared__ uint32_t key[ONE_WG], place[ONE_WG], count[SW][BINS], part[SW];
-  constexpr int G = ONE_WG / (64 * SW);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
-  const int per = (n + 64 * SW - 1) / (64 * SW);   // groups of 64 for each wavefront
-  uint32_t k[G], p[G], r[G];
+__global__ void __launch_bounds__(RB) k_rank(const ID* ids, int n, int64_t vocab, uint32_t* key_out, uint32_t* place_out) {
+  typedef uint32_t four __attribute__((ext_vector_type(4)));
+  __shared__ __align__(16) uint32_t key[PARTS * PART];
+  __shared__ uint32_t count[PARTS][RANKED];
+  const int tid = threadIdx.x, e0 = tid % (RANKED / PER_LANE) * PER_LANE, part = tid / (RANKED / PER_LANE);
+  const int per = (n + 4 * PARTS - 1) / (4 * PARTS) * 4, padded = per * PARTS;   // ids of a part, of all
+  uint32_t k[FEW / RB];
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const int i = (wave * per + g) * 64 + lane;
-    k[g] = g < per && i < n ? id_key(ids[i], vocab) : 0;
-    p[g] = (uint32_t)i;
+  for (int r = 0; r < FEW / RB; ++r) {
+    const int j = r * RB + tid;
+    k[r] = j < n ? id_key(ids[j], vocab) : 0xFFFFFFFFu;
   }
-  for (int pass = 0; pass < passes; ++pass) {
-    for (int i = tid; i < SW * BINS; i += 64 * SW) (&count[0][0])[i] = 0;
-    __syncthreads();
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const bool mine = g < per && (wave * per + g) * 64 + lane < n;
-      if (g < per) r[g] = place_in_wave(k[g] >> pass * width & ((1u << width) - 1), mine, width, count[wave]);
-    }
-    __syncthreads();
-    // the first place of each digit's tokens of each wavefront: two threads to a digit, eight wavefronts each
-    static_assert(BINS * 2 == 64 * SW, "two threads to a digit");
-    uint32_t c[SW / 2], s = 0;
+  for (int r = 0; r < FEW / RB; ++r) {
+    const int j = r * RB + tid;
+    if (j < padded) key[j / per * PART + j % per] = k[r];
+  }
+  const int i0 = (int)blockIdx.x * RANKED + e0, from = part * per;
+  uint32_t id[PER_LANE], before[PER_LANE] = {};
 #pragma unroll
-    for (int w = 0; w < SW / 2; ++w) {
-      c[w] = count[(tid & 1) * (SW / 2) + w][tid >> 1];
-      s += c[w];
-    }
-    uint32_t at = sum_before<SW>(s, part);
+  for (int e = 0; e < PER_LANE; ++e) id[e] = i0 + e < n ? id_key(ids[i0 + e], vocab) : 0;
+  __syncthreads();
+  const uint32_t* own = key + part * PART;
+  if (!__any(i0 + PER_LANE > from && i0 < from + per)) {
+    uint32_t bar[PER_LANE];
 #pragma unroll
-    for (int w = 0; w < SW / 2; ++w) {
-      count[(tid & 1) * (SW / 2) + w][tid >> 1] = at;
-      at += c[w];
-    }
-    __syncthreads();
-    const bool last = pass + 1 == passes;
+    for (int e = 0; e < PER_LANE; ++e) bar[e] = id[e] + (i0 >= from);   // (of equal ids the earlier come first)
+    for (int j = 0; j < per; j += 4) {
+      const four q = *(const four*)(own + j);
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      if (!(g < per && (wave * per + g) * 64 + lane < n)) continue;
-      const uint32_t to = count[wave][k[g] >> pass * width & ((1u << width) - 1)] + r[g];
-      (last ? key_out : key)[to] = k[g];
-      (last ? place_out : place)[to] = p[g];
-    }
-    __syncthreads();
-    if (last) break;
+      for (int h = 0; h < 4; ++h)
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const int i = (wave * per + g) * 64 + lane;
-      if (!(g < per && i < n)) continue;
-      k[g] = key[i];
-      p[g] = place[i];
+        for (int e = 0; e < PER_LANE; ++e) before[e] += q[h] < bar[e];
     }
-    // (the next pass writes key and place only behind barriers)
+  } else {
+    for (int j = 0; j < per; ++j) {
+      const uint32_t q = own[j];
+#pragma unroll
+      for (int e = 0; e < PER_LANE; ++e) before[e] += q < id[e] + (from + j < i0 + e);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < PER_LANE; ++e) count[part][e0 + e] = before[e];
+  __syncthreads();
+  const int i = (int)blockIdx.x * RANKED + tid;
+  if (tid < RANKED && i < n) {
+    uint32_t to = 0;
+#pragma unroll 8
+    for (int p = 0; p < PARTS; ++p) to += count[p][tid];
+    key_out[to] = id_key(ids[i], vocab);
+    place_out[to] = (uint32_t)i;
   }
 }
 
@@ -213,16 +225,18 @@ k_scatter(const void* in, const uint32_t* place_in, int64_t n, int64_t vocab, in
   for (int i = tid; i < EW * BINS; i += EB) (&count[0][0])[i] = 0;
   const int64_t i0 = (int64_t)blockIdx.x * TILE + wave * (TILE / EW) + lane;
   const uint32_t mask = (1u << width) - 1;
-  uint32_t k[G], p[G], r[G];
+  uint32_t k[G], p[G], r[G], digit[G];
+  bool mine[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     const int64_t i = i0 + g * 64;
-    k[g] = i < n ? key_at<ID, FIRST>(in, i, vocab) : 0;
-    p[g] = FIRST || i >= n ? (uint32_t)i : place_in[i];
+    mine[g] = i < n;
+    k[g] = mine[g] ? key_at<ID, FIRST>(in, i, vocab) : 0;
+    p[g] = FIRST || !mine[g] ? (uint32_t)i : place_in[i];
+    digit[g] = k[g] >> shift & mask;
   }
   __syncthreads();
-#pragma unroll
-  for (int g = 0; g < G; ++g) r[g] = place_in_wave(k[g] >> shift & mask, i0 + g * 64 < n, width, count[wave]);
+  places_in_wave<G>(digit, mine, count[wave], r);
   __syncthreads();
   // the first place of each digit's tokens of each wavefront: two digits to a thread
   static_assert(BINS == 2 * EB, "two digits to a thread");
@@ -245,8 +259,8 @@ k_scatter(const void* in, const uint32_t* place_in, int64_t n, int64_t vocab, in
   __syncthreads();
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    if (i0 + g * 64 >= n) continue;
-    const uint32_t to = count[wave][k[g] >> shift & mask] + r[g];
+    if (!mine[g]) continue;
+    const uint32_t to = count[wave][digit[g]] + r[g];
     key_out[to] = k[g];
     place_out[to] = p[g];
   }
@@ -260,59 +274,71 @@ k_scatter(const void* in, const uint32_t* place_in, int64_t n, int64_t vocab, in
 // each row of gradients is read once, in whole cache lines.
 struct Sorted { const uint32_t *key, *place; int64_t n; int chunk; float* part; };   // part [chunk][2][dim]
 
-template <class O>
-__device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t id, int64_t j, float (&s)[EV], int have) {
-  O* out = (O*)a.d_table + id * a.dim + j;
+// EV columns as they lie in memory.
+template <class T> struct Columns {
+  Sixteen<T> q[EV / Sixteen<T>::V];
+  __device__ __forceinline__ void load(const T* p, int have) {
+    if (have == EV) {
 #pragma unroll
-  for (int e = 0; e < EV; ++e) s[e] *= a.scale;
-  if (a.add) {
-    float f[EV];
-    read_columns<O, EV>(f, out, have);
+      for (int i = 0; i < EV / Sixteen<T>::V; ++i) q[i].load(p + i * Sixteen<T>::V);
+    } else {
+      float f[EV];
+      read_columns<T, EV>(f, p, have);
 #pragma unroll
-    for (int e = 0; e < EV; ++e) s[e] += f[e];
+      for (int i = 0; i < EV / Sixteen<T>::V; ++i) {
+        float part[Sixteen<T>::V];
+#pragma unroll
+        for (int e = 0; e < Sixteen<T>::V; ++e) part[e] = f[i * Sixteen<T>::V + e];
+        q[i].put(part);
+      }
+    }
   }
-  write_columns<O, EV>(out, s, have);
+  __device__ __forceinline__ float get(int e) const { return q[e / Sixteen<T>::V].get(e % Sixteen<T>::V); }
+};
+
+// was: the row before (ADD)
+template <class O, bool ADD>
+__device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t id, int64_t j, float (&s)[EV], const Columns<O>& was, int have) {
+#pragma unroll
+  for (int e = 0; e < EV; ++e) s[e] = ADD ? was.get(e) + s[e] * a.scale : s[e] * a.scale;
+  write_columns<O, EV>((O*)a.d_table + id * a.dim + j, s, have);
 }
 
-template <class T, class O>
+template <class T, class O, bool ADD>
 __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& s, int64_t c, int64_t j) {
-  constexpr int B = 8;   // rows under way
+  constexpr int B = ADD ? 4 : 8;   // rows under way, with ADD the rows of the table that they end in as well
   const int lane = threadIdx.x & 63;
   const int have = a.dim - j >= EV ? EV : a.dim > j ? (int)(a.dim - j) : 0;
   const int64_t lo = c * s.chunk, hi = lo + s.chunk < s.n ? lo + s.chunk : s.n;
-  bool began_before = lo > 0 && s.key[lo - 1] == s.key[lo];
+  const uint32_t first = s.key[lo], ahead = lo > 0 ? s.key[lo - 1] : 0xFFFFFFFFu;
+  bool began_before = first == ahead;
   float acc[EV] = {};
-  auto part = [&](int which) {
-    write_columns<float, EV>(s.part + (2 * c + which) * a.dim + j, acc, have);
-#pragma unroll
-    for (int e = 0; e < EV; ++e) acc[e] = 0.f;
-  };
   for (int64_t k0 = lo; k0 < hi; k0 += 64) {
     const int64_t k = k0 + lane;
     const uint32_t key = k < hi ? s.key[k] : (uint32_t)a.vocab, place = k < hi ? s.place[k] : 0;
     const uint32_t next = k + 1 < s.n ? s.key[k + 1] : 0xFFFFFFFFu;
     for (int b0 = 0; b0 < 64; b0 += B) {
-      float row[B][EV];
+      Columns<T> row[B];
+      Columns<O> was[ADD ? B : 1];
 #pragma unroll
       for (int b = 0; b < B; ++b) {
         const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)key, b0 + b), at = (uint32_t)__builtin_amdgcn_readlane((int)place, b0 + b);
-        if (id < (uint64_t)a.vocab) read_columns<T, EV>(row[b], (const T*)a.d_out + (int64_t)at * a.dim + j, have);
+        if (id >= (uint64_t)a.vocab) continue;
+        row[b].load((const T*)a.d_out + (int64_t)at * a.dim + j, have);
+        if (ADD && (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id) was[b].load((const O*)a.d_table + (int64_t)id * a.dim + j, have);
       }
 #pragma unroll
       for (int b = 0; b < B; ++b) {
         const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)key, b0 + b);
         if (id >= (uint64_t)a.vocab) return;   // the end of the chunk, or of the tokens that count
 #pragma unroll
-        for (int e = 0; e < EV; ++e) acc[e] += row[b][e];
+        for (int e = 0; e < EV; ++e) acc[e] += row[b].get(e);
         const bool ends = (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id;
         if (!ends && k0 + b0 + b + 1 < hi) continue;
-        if (ends && !began_before) {
-          put_row<O>(a, id, j, acc, have);
+        if (ends && !began_before) put_row<O, ADD>(a, id, j, acc, was[ADD ? b : 0], have);
+        else write_columns<float, EV>(s.part + (2 * c + (began_before ? 0 : 1)) * a.dim + j, acc, have);
 #pragma unroll
-          for (int e = 0; e < EV; ++e) acc[e] = 0.f;
-        } else {
-          part(began_before ? 0 : 1);
-        }
+        for (int e = 0; e < EV; ++e) acc[e] = 0.f;
         began_before = false;
       }
     }
@@ -340,24 +366,25 @@ template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArg
   }
 }
 
-template <class T, class O>
+template <class T, class O, bool ADD>
 __global__ void __launch_bounds__(EB) k_sums(const EmbedGradArgs a, const Sorted s, int64_t pieces, int slices, int64_t clears) {
   for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces + clears; p += (int64_t)gridDim.x * EW) {
-    if (p >= pieces) clear_rows<O>(a, s, (p - pieces) * EMPTY_ROWS);
-    else sum_chunk<T, O>(a, s, p / slices, (p % slices) * SLICE + (threadIdx.x & 63) * EV);
+    const int64_t q = p - clears;   // (rows to clear first: their searches wait for one load after the other)
+    if (q < 0) clear_rows<O>(a, s, p * EMPTY_ROWS);
+    else sum_chunk<T, O, ADD>(a, s, q / slices, (q % slices) * SLICE + (threadIdx.x & 63) * EV);
   }
 }
 
 // The id that starts in a chunk and goes on beyond it: its part of the chunk and those of the chunks behind, dealt out to the
 // wavefronts of a workgroup.
-template <class O>
+template <class O, bool ADD>
 __global__ void __launch_bounds__(EB) k_join(const EmbedGradArgs a, const Sorted s, int64_t chunks) {
   __shared__ float sums[EW][SLICE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = blockIdx.x, lo = c * s.chunk, hi = lo + s.chunk;
   if (hi >= s.n) return;
-  const uint32_t id = s.key[hi - 1];
-  if (id >= (uint64_t)a.vocab || s.key[hi] != id || (s.key[lo] == id && lo > 0 && s.key[lo - 1] == id)) return;
+  const uint32_t id = s.key[hi - 1], then = s.key[hi], first = s.key[lo], before = lo > 0 ? s.key[lo - 1] : 0xFFFFFFFFu;
+  if (id >= (uint64_t)a.vocab || then != id || (first == id && before == id)) return;
   int64_t behind = 0;   // chunks behind this one that go on with the id
   for (;;) {
     const int64_t at = (c + 1 + behind + lane) * s.chunk;
@@ -369,6 +396,8 @@ __global__ void __launch_bounds__(EB) k_join(const EmbedGradArgs a, const Sorted
     const int64_t j = j0 + lane * EV;
     const int have = a.dim - j >= EV ? EV : a.dim > j ? (int)(a.dim - j) : 0;
     float acc[EV] = {};
+    Columns<O> was;
+    if (ADD && wave == 0) was.load((const O*)a.d_table + (int64_t)id * a.dim + j, have);
 #pragma unroll 4
     for (int64_t k = wave; k <= behind; k += EW) {
       float f[EV];
@@ -383,7 +412,7 @@ __global__ void __launch_bounds__(EB) k_join(const EmbedGradArgs a, const Sorted
       for (int w = 1; w < EW; ++w)
 #pragma unroll
         for (int e = 0; e < EV; ++e) acc[e] += sums[w][e * 64 + lane];
-      put_row<O>(a, id, j, acc, have);
+      put_row<O, ADD>(a, id, j, acc, was, have);
     }
     __syncthreads();
   }
@@ -406,7 +435,7 @@ struct Layout { int64_t key[2], place[2], counts, total, part, bytes, tiles; };
 Layout layout(int64_t n, int64_t dim) {
   Layout l = {};
   auto take = [&](int64_t bytes) { const int64_t at = l.bytes; l.bytes += (bytes + 255) / 256 * 256; return at; };
-  const bool big = n > ONE_WG;
+  const bool big = n > FEW;
   l.tiles = (n + TILE - 1) / TILE;
   for (int i = 0; i < (big ? 2 : 1); ++i) {
     l.key[i] = take(4 * n);
@@ -442,8 +471,8 @@ void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int i
   int from = 0;
   if (a.n > 0) with_id(id_bits, [&](auto id) {
     using ID = decltype(id);
-    if (a.n <= ONE_WG) {
-      hipLaunchKernelGGL((k_sort<ID>), dim3(1), dim3(64 * SW), 0, s, (const ID*)a.ids, (int)a.n, a.vocab, width, passes, at(l.key[0]), at(l.place[0]));
+    if (a.n <= FEW) {
+      hipLaunchKernelGGL((k_rank<ID>), dim3((unsigned)((a.n + RANKED - 1) / RANKED)), dim3(RB), 0, s, (const ID*)a.ids, (int)a.n, a.vocab, at(l.key[0]), at(l.place[0]));
       return;
     }
     const dim3 grid((unsigned)l.tiles);
@@ -461,11 +490,12 @@ void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int i
   const int chunk = chunk_of(a.n);
   const int64_t chunks = (a.n + chunk - 1) / chunk, slices = in_slices(a.dim), clears = a.add ? 0 : (a.vocab + EMPTY_ROWS - 1) / EMPTY_ROWS;
   const Sorted sorted = {at(l.key[from]), at(l.place[from]), a.n, chunk, (float*)at(l.part)};
-  with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) {
-    hipLaunchKernelGGL((k_sums<decltype(t), decltype(o)>), groups_for(chunks * slices + clears), dim3(EB), 0, s, a, sorted, chunks * slices, (int)slices, clears);
+  with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) { with_flag(a.add != 0, [&](auto add) {
+    constexpr bool ADD = decltype(add)::value;
+    hipLaunchKernelGGL((k_sums<decltype(t), decltype(o), ADD>), groups_for(chunks * slices + clears), dim3(EB), 0, s, a, sorted, chunks * slices, (int)slices, clears);
     if (chunks > 1)
-      hipLaunchKernelGGL((k_join<decltype(o)>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(EB), 0, s, a, sorted, chunks);
-  }); });
+      hipLaunchKernelGGL((k_join<decltype(o), ADD>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(EB), 0, s, a, sorted, chunks);
+  }); }); });
 }
 
 }  // namespace pb

@@ -1,8 +1,6 @@
 // Log probabilities of given tokens, entropies, top alternatives (pb_log_probs) and their gradient (pb_log_probs_backward).
 #include <math.h>
 
-#include <type_traits>
-
 #include "pb_ops.h"
 #include "pb_wave.h"
 
@@ -369,8 +367,6 @@ int64_t logp_workspace(int64_t rows, int64_t vocab, int top) {
   const Split s = split(rows, vocab);
   return s.parts > 1 ? rows * s.parts * (int64_t)part_bytes(top) : 0;
 }
-
-template <class F> void with_flag(bool b, F&& f) { b ? f(std::true_type()) : f(std::false_type()); }
 
 void launch_logp(const LogpArgs& a, int dtype, int id_bits, hipStream_t s) {
   const Split sp = split(a.rows, a.vocab);

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/pb.h"
 
 namespace pb {
@@ -151,6 +153,7 @@ template <class T> struct Sixteen {
 
 // f(T{}, U{}) with the C++ types of two pb_dtype
 template <class F> void with_type(int t, F&& f) { t == PB_BF16 ? f(bf16()) : f(float()); }
+template <class F> void with_flag(bool b, F&& f) { b ? f(std::true_type()) : f(std::false_type()); }
 template <class F> void with_id(int bits, F&& f) { bits == 64 ? f(int64_t()) : f(int32_t()); }
 #endif
 
