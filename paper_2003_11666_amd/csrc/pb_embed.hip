@@ -122,57 +122,66 @@ template <int WAVES> __device__ __forceinline__ uint32_t sum_before(uint32_t x, 
 // for 64 comparisons and an LDS read for sixteen times as many (with one token to a lane these reads were the bound).  The 67
 // million comparisons of 8192 tokens take the chip 3.4 us; a radix sort in one workgroup took 31 us, one in tiles takes six
 // launches.
-constexpr int RANKED = 32, PER_LANE = 4, RB = 1024, PARTS = RB * PER_LANE / RANKED, PART = FEW / PARTS + 4;   // (4 words on: other banks)
+constexpr int RANKED = 32, PER_LANE = 4, RB = 1024, PARTS = RB * PER_LANE / RANKED;
+__device__ __forceinline__ int spread(int j) { return j + (j >> 5) * 4; }   // (parts start at other banks)
 template <class ID>
 __global__ void __launch_bounds__(RB) k_rank(const ID* ids, int n, int64_t vocab, uint32_t* key_out, uint32_t* place_out) {
   typedef uint32_t four __attribute__((ext_vector_type(4)));
-  __shared__ __align__(16) uint32_t key[PARTS * PART];
-  __shared__ uint32_t count[PARTS][RANKED];
+  __shared__ __align__(16) uint32_t key[FEW + FEW / 8];
+  __shared__ uint32_t count[RB / 64][RANKED];
   const int tid = threadIdx.x, e0 = tid % (RANKED / PER_LANE) * PER_LANE, part = tid / (RANKED / PER_LANE);
   const int per = (n + 4 * PARTS - 1) / (4 * PARTS) * 4, padded = per * PARTS;   // ids of a part, of all
-  uint32_t k[FEW / RB];
+  for (int j0 = 0; j0 < padded; j0 += 8 * RB) {
+    ID k[8];   // (eight loads under way, none behind a branch)
 #pragma unroll
-  for (int r = 0; r < FEW / RB; ++r) {
-    const int j = r * RB + tid;
-    k[r] = j < n ? id_key(ids[j], vocab) : 0xFFFFFFFFu;
-  }
+    for (int r = 0; r < 8; ++r) {
+      const int j = j0 + r * RB + tid;
+      k[r] = ids[j < n ? j : n - 1];
+    }
 #pragma unroll
-  for (int r = 0; r < FEW / RB; ++r) {
-    const int j = r * RB + tid;
-    if (j < padded) key[j / per * PART + j % per] = k[r];
+    for (int r = 0; r < 8; ++r) {
+      const int j = j0 + r * RB + tid;
+      if (j < padded) key[spread(j)] = j < n ? id_key(k[r], vocab) : 0xFFFFFFFFu;
+    }
   }
   const int i0 = (int)blockIdx.x * RANKED + e0, from = part * per;
   uint32_t id[PER_LANE], before[PER_LANE] = {};
 #pragma unroll
-  for (int e = 0; e < PER_LANE; ++e) id[e] = i0 + e < n ? id_key(ids[i0 + e], vocab) : 0;
+  for (int e = 0; e < PER_LANE; ++e) id[e] = id_key(ids[i0 + e < n ? i0 + e : n - 1], vocab);
   __syncthreads();
-  const uint32_t* own = key + part * PART;
   if (!__any(i0 + PER_LANE > from && i0 < from + per)) {
     uint32_t bar[PER_LANE];
 #pragma unroll
     for (int e = 0; e < PER_LANE; ++e) bar[e] = id[e] + (i0 >= from);   // (of equal ids the earlier come first)
-    for (int j = 0; j < per; j += 4) {
-      const four q = *(const four*)(own + j);
+#pragma unroll 2
+    for (int j = from; j < from + per; j += 4) {
+      const four q = *(const four*)(key + spread(j));
 #pragma unroll
       for (int h = 0; h < 4; ++h)
 #pragma unroll
         for (int e = 0; e < PER_LANE; ++e) before[e] += q[h] < bar[e];
     }
   } else {
-    for (int j = 0; j < per; ++j) {
-      const uint32_t q = own[j];
+    for (int j = from; j < from + per; j += 4) {
+      const four q = *(const four*)(key + spread(j));
 #pragma unroll
-      for (int e = 0; e < PER_LANE; ++e) before[e] += q < id[e] + (from + j < i0 + e);
+      for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int e = 0; e < PER_LANE; ++e) before[e] += q[h] < id[e] + (j + h < i0 + e);
     }
   }
 #pragma unroll
-  for (int e = 0; e < PER_LANE; ++e) count[part][e0 + e] = before[e];
+  for (int e = 0; e < PER_LANE; ++e) {
+#pragma unroll
+    for (int o = RANKED / PER_LANE; o < 64; o *= 2) before[e] += (uint32_t)__shfl_xor((int)before[e], o, 64);   // the wavefront's parts
+    if ((tid & 63) < RANKED / PER_LANE) count[tid / 64][e0 + e] = before[e];
+  }
   __syncthreads();
   const int i = (int)blockIdx.x * RANKED + tid;
   if (tid < RANKED && i < n) {
     uint32_t to = 0;
-#pragma unroll 8
-    for (int p = 0; p < PARTS; ++p) to += count[p][tid];
+#pragma unroll
+    for (int w = 0; w < RB / 64; ++w) to += count[w][tid];
     key_out[to] = id_key(ids[i], vocab);
     place_out[to] = (uint32_t)i;
   }
