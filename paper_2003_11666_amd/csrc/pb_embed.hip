@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a, int64_t pieces,
 // Stable, by digits of the id from the lowest up; an id outside the table becomes `vocab`, behind all others.  Digits are as
 // wide as the fewest passes make them, 9 bits at most: two passes for up to 2^18 ids.
 constexpr int DIGIT = 9, BINS = 1 << DIGIT;
-constexpr int FEW = 16384;          // up to so many tokens are ranked by comparisons
+constexpr int FEW = 8192;           // up to so many tokens are ranked by comparisons
 constexpr int TILE = 1024;          // tokens per workgroup of a pass over more
 template <class ID> __device__ __forceinline__ uint32_t id_key(ID id, int64_t vocab) { return (uint32_t)(id >= 0 && (int64_t)id < vocab ? (int64_t)id : vocab); }
 
@@ -286,10 +286,10 @@ struct Sorted { const uint32_t *key, *place; int64_t n; int chunk; float* part; 
 // EV columns as they lie in memory.
 template <class T> struct Columns {
   Sixteen<T> q[EV / Sixteen<T>::V];
-  __device__ __forceinline__ void load(const T* p, int have) {
+  template <bool ONCE = false> __device__ __forceinline__ void load(const T* p, int have) {
     if (have == EV) {
 #pragma unroll
-      for (int i = 0; i < EV / Sixteen<T>::V; ++i) q[i].load(p + i * Sixteen<T>::V);
+      for (int i = 0; i < EV / Sixteen<T>::V; ++i) q[i].template load<ONCE>(p + i * Sixteen<T>::V);
     } else {
       float f[EV];
       read_columns<T, EV>(f, p, have);
@@ -333,7 +333,7 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& 
       for (int b = 0; b < B; ++b) {
         const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)key, b0 + b), at = (uint32_t)__builtin_amdgcn_readlane((int)place, b0 + b);
         if (id >= (uint64_t)a.vocab) continue;
-        row[b].load((const T*)a.d_out + (int64_t)at * a.dim + j, have);
+        row[b].template load<true>((const T*)a.d_out + (int64_t)at * a.dim + j, have);
         if (ADD && (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id) was[b].load((const O*)a.d_table + (int64_t)id * a.dim + j, have);
       }
 #pragma unroll

@@ -160,7 +160,7 @@ __device__ __forceinline__ void scan(const T* x, uint32_t lo, uint32_t hi, uint3
 #pragma unroll
     for (uint32_t i = 0; i < U; ++i) {
       const uint32_t j = j0 + i * waves * 64 * V;
-      if (j < whole) q[i].load(x + j);
+      if (j < whole) q[i].template load<true>(x + j);
     }
     float high = -INFINITY;
 #pragma unroll
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t 
     Sixteen<T> q[U];
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (j0 + (i * 64 + 1) * V <= vocab) q[i].load(x + j0 + i * 64 * V);
+      if (j0 + (i * 64 + 1) * V <= vocab) q[i].template load<true>(x + j0 + i * 64 * V);
     const float m = a.norm[2 * r], ls = a.norm[2 * r + 1], ref = against(m);
     const int64_t t = a.g_logp ? (int64_t)((const ID*)a.targets)[r] : -1;
     const float gl = t >= 0 && t < vocab ? a.g_logp[r] : 0.f;
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t 
 #pragma unroll
         for (int e = 0; e < V; ++e) y[e] = grad(q[i].get(e), j + e);
         q[i].put(y);
-        q[i].store(d + j);
+        q[i].template store<true>(d + j);
       } else {
         for (uint32_t e = j; e < vocab; ++e) d[e] = from_float<T>(grad(to_float(x[e]), e));
       }

@@ -137,8 +137,15 @@ template <class T> struct Sixteen {
   typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
   static constexpr int V = 16 / sizeof(T);
   words q;
-  __device__ __forceinline__ void load(const T* p) { q = __builtin_nontemporal_load((const loose*)p); }
-  __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store((loose)q, (loose*)p); }
+  // ONCE: read or written once by the whole launch and not soon again, so not to be kept in a cache
+  template <bool ONCE = false> __device__ __forceinline__ void load(const T* p) {
+    if constexpr (ONCE) q = __builtin_nontemporal_load((const loose*)p);
+    else q = *(const loose*)p;
+  }
+  template <bool ONCE = false> __device__ __forceinline__ void store(T* p) const {
+    if constexpr (ONCE) __builtin_nontemporal_store((loose)q, (loose*)p);
+    else *(loose*)p = (loose)q;
+  }
   __device__ __forceinline__ float get(int e) const {
     const uint32_t w = q[e * sizeof(T) / 4];
     return __uint_as_float(sizeof(T) == 4 ? w : e % 2 ? w & 0xFFFF0000u : w << 16);
