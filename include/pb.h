@@ -337,8 +337,9 @@ typedef struct {
 /* Entries of the flat moment arrays for tensors of n[0..n_tensors-1] elements. */
 int64_t pb_adamw_elements(const int64_t* n, int32_t n_tensors);
 
-/* m, v (and m_exp, v_exp where moment_bits = 8; NULL otherwise) on 16-byte boundaries; the tensors
- * on boundaries of their element size (16 bytes is faster).  Entries between two tensors: 8-bit ones
+/* m, v (and m_exp, v_exp where moment_bits = 8; NULL otherwise): m and v on 16-byte boundaries; the tensors
+ * on boundaries of their element size (16 bytes is faster).  What is written must not overlap: a tensor that is
+ * listed twice is refused.  A gradient must not overlap it either (not checked).  Entries between two tensors: 8-bit ones
  * are written as 0, 32-bit ones left as they are.  step_dev counting from values below 1 gives NaN. */
 int pb_adamw_step(const pb_adamw_tensor* tensors, int32_t n_tensors, const pb_adamw_desc* desc, void* m, void* v,
                   uint8_t* m_exp, uint8_t* v_exp, void* stream);
@@ -386,7 +387,7 @@ int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const
 /* Gradient of the table: for each row, scale * the sum of the rows of d_out (n rows of dim, type `dtype`) whose
  * id is that row's, added up in 32 bits in the order of their places.  add = 0: d_table (vocab rows of dim, type
  * table_dtype) is written, with zeros in rows that no id names; add = 1: the sums are added to it, and rows that no
- * id names are left alone.  n <= 2^30, vocab <= 2^31.  `workspace`: pb_embed_backward_workspace bytes, 16-byte
+ * id names are left alone.  d_out and d_table must not overlap.  n <= 2^30, vocab <= 2^31.  `workspace`: pb_embed_backward_workspace bytes, 16-byte
  * aligned, free for other use when the call's work is done. */
 int64_t pb_embed_backward_workspace(int64_t n, int64_t vocab, int64_t dim);
 int pb_embed_backward(const void* d_out, int32_t dtype, const void* ids, int32_t id_bits, int64_t n, int64_t vocab,

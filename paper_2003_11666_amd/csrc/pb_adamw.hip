@@ -179,7 +179,12 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
     const int64_t i = i0 + u * AT * V, at = at0 + u * AT * V;
     if (!inside(u)) continue;
     bool plain = false;
-    if constexpr (BITS == 8) plain = a.approx && __all(vec && i + V <= n && plain_exponent(x[u % A].em) && plain_exponent(x[u % A].ev));
+    if constexpr (BITS == 8) {
+      const Vector<W, G, BITS, V>& y = x[u % A];
+      const bool m_fits = plain_exponent(y.em) || (y.em == 0 && (y.m.q[0][0] | y.m.q[0][1]) == 0);   // (or a vector of zeros: a weight that never had a gradient)
+      const bool v_fits = plain_exponent(y.ev) || (y.ev == 0 && (y.v.q[0][0] | y.v.q[0][1]) == 0);
+      plain = a.approx && __all(vec && i + V <= n && m_fits && v_fits);
+    }
     if (BITS == 8 && plain) update(std::true_type(), x[u % A], u);
     else update(std::false_type(), x[u % A], u);
     if (u + A < U) request(x[u % A], u + A);
@@ -216,10 +221,13 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
         }
       }
     } else {
-      const int m_top = block_exponent(row_max(tm)), v_top = block_exponent(row_max(tv));
+      tm = row_max(tm);
+      tv = row_max(tv);
+      const int m_top = block_exponent(tm), v_top = block_exponent(tv);
       Vec<uint8_t, V> mq, vq;
       auto encode = [&](auto P) {
         constexpr bool PLAIN = decltype(P)::value;
+        const int e_m = PLAIN && tm == 0 ? TOP_V + 1 : m_top, e_v = PLAIN && tv == 0 ? TOP_V + 1 : v_top;   // (of a block of zeros: any that gives them code 0)
         uint32_t m2[2] = {0, 0}, v2[2] = {0, 0};
         const uint64_t count = key + (uint64_t)(at >> 1) * GOLDEN;
 #pragma unroll
@@ -228,13 +236,13 @@ __global__ void __launch_bounds__(AT) k_adamw(const AdamWArgs a) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint32_t r = (uint32_t)(z >> 32 * h);
-            m2[e / 4] |= encode_m<PLAIN>(mv[e + h], (r & 0xFFFF) << 4 | 8, m_top) << 8 * ((e + h) % 4);
-            v2[e / 4] |= encode_v<PLAIN>(vv[e + h], (r >> 12 & 0xFFFF0) | 8, v_top) << 8 * ((e + h) % 4);
+            m2[e / 4] |= encode_m<PLAIN>(mv[e + h], (r & 0xFFFF) << 4 | 8, e_m) << 8 * ((e + h) % 4);
+            v2[e / 4] |= encode_v<PLAIN>(vv[e + h], (r >> 12 & 0xFFFF0) | 8, e_v) << 8 * ((e + h) % 4);
           }
         }
         mq.q[0][0] = m2[0]; mq.q[0][1] = m2[1]; vq.q[0][0] = v2[0]; vq.q[0][1] = v2[1];
       };
-      if (__all(plain_exponent(m_top) && plain_exponent(v_top))) encode(std::true_type());
+      if (__all((tm == 0 || plain_exponent(m_top)) && (tv == 0 || plain_exponent(v_top)))) encode(std::true_type());
       else encode(std::false_type());
       mq.store((uint8_t*)a.m + at);
       vq.store((uint8_t*)a.v + at);

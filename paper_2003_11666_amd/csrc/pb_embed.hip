@@ -432,7 +432,7 @@ namespace {
 
 dim3 groups_for(int64_t wavefronts) {
   const int64_t g = (wavefronts + EW - 1) / EW;
-  return dim3((unsigned)(g < (1 << 20) ? g : 1 << 20));
+  return dim3((unsigned)(g < MAX_GROUPS ? g : MAX_GROUPS));
 }
 
 int64_t in_slices(int64_t dim) { return (dim + SLICE - 1) / SLICE; }

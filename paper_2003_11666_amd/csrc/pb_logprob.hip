@@ -245,33 +245,38 @@ __host__ __device__ __forceinline__ size_t part_bytes(int top) { return 16 + 8 *
 
 // Bound by memory: a row is read once.  A row to a wavefront (short ones), to a workgroup, or in `parts` of `part` logits to a
 // workgroup each.
-template <class T, class ID, bool TOP, bool SHORT>
-__global__ void __launch_bounds__(LB) k_logp(const LogpArgs a, int parts, int part) {
-  __shared__ JoinLds lds;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t r = SHORT ? (int64_t)blockIdx.x * WAVES + wave : blockIdx.x / parts;
-  if (SHORT && r >= a.rows) return;
-  const T* x = (const T*)a.logits + r * a.stride;
-  Sums w = NOTHING;
-  Best best(a.top, lds.key[wave]);
-  if (SHORT) {
-    scan<T, TOP>(x, 0, (uint32_t)a.vocab, 0, 1, a.scale, w, best);
+template <class T, class ID, bool TOP>
+__global__ void __launch_bounds__(LB) k_logp_short(const LogpArgs a) {
+  __shared__ uint64_t lds[WAVES][128];
+  const int wave = threadIdx.x >> 6;
+  for (int64_t r = (int64_t)blockIdx.x * WAVES + wave; r < a.rows; r += (int64_t)gridDim.x * WAVES) {
+    Sums w = NOTHING;
+    Best best(a.top, lds[wave]);
+    scan<T, TOP>((const T*)a.logits + r * a.stride, 0, (uint32_t)a.vocab, 0, 1, a.scale, w, best);
     join_lanes(w);
     if (TOP) best.finish();
     give<T, ID>(a, r, w, best);
-    return;
   }
-  const int64_t lo = (int64_t)(blockIdx.x % parts) * part;
-  scan<T, TOP>(x, (uint32_t)lo, (uint32_t)(a.vocab - lo < part ? a.vocab : lo + part), wave, WAVES, a.scale, w, best);
-  join_waves<TOP>(w, best, lds);
-  if (wave) return;
-  if (parts == 1) {
-    give<T, ID>(a, r, w, best);
-    return;
+}
+
+template <class T, class ID, bool TOP>
+__global__ void __launch_bounds__(LB) k_logp(const LogpArgs a, int parts, int part) {
+  __shared__ JoinLds lds;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int64_t p = blockIdx.x; p < a.rows * parts; p += gridDim.x) {
+    const int64_t r = p / parts, lo = (p - r * parts) * part;
+    Sums w = NOTHING;
+    Best best(a.top, lds.key[wave]);
+    scan<T, TOP>((const T*)a.logits + r * a.stride, (uint32_t)lo, (uint32_t)(a.vocab - lo < part ? a.vocab : lo + part), wave, WAVES, a.scale, w, best);
+    join_waves<TOP>(w, best, lds);
+    if (wave == 0) {
+      char* at = (char*)a.workspace + p * part_bytes(a.top);
+      if (parts == 1) give<T, ID>(a, r, w, best);
+      else if (lane == 0) *(Sums*)at = w;
+      if (TOP && parts > 1 && lane < a.top) ((uint64_t*)(at + 16))[lane] = best.key;
+    }
+    if (p + gridDim.x < a.rows * parts) __syncthreads();   // (before the next one's LDS)
   }
-  char* at = (char*)a.workspace + blockIdx.x * part_bytes(a.top);
-  if (lane == 0) *(Sums*)at = w;
-  if (TOP && lane < a.top) ((uint64_t*)(at + 16))[lane] = best.key;
 }
 
 template <class T, class ID, bool TOP>
@@ -368,16 +373,18 @@ int64_t logp_workspace(int64_t rows, int64_t vocab, int top) {
   return s.parts > 1 ? rows * s.parts * (int64_t)part_bytes(top) : 0;
 }
 
+static dim3 groups_for(int64_t n) { return dim3((unsigned)(n < MAX_GROUPS ? n : MAX_GROUPS)); }
+
 void launch_logp(const LogpArgs& a, int dtype, int id_bits, hipStream_t s) {
   const Split sp = split(a.rows, a.vocab);
   with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) { with_flag(a.top > 0, [&](auto top) {
     using T = decltype(t); using ID = decltype(id);
     constexpr bool TOP = decltype(top)::value;
     if (a.vocab <= SHORT_ROW) {
-      hipLaunchKernelGGL((k_logp<T, ID, TOP, true>), dim3((unsigned)((a.rows + WAVES - 1) / WAVES)), dim3(LB), 0, s, a, 1, (int)a.vocab);
+      hipLaunchKernelGGL((k_logp_short<T, ID, TOP>), groups_for((a.rows + WAVES - 1) / WAVES), dim3(LB), 0, s, a);
       return;
     }
-    hipLaunchKernelGGL((k_logp<T, ID, TOP, false>), dim3((unsigned)(a.rows * sp.parts)), dim3(LB), 0, s, a, sp.parts, sp.part);
+    hipLaunchKernelGGL((k_logp<T, ID, TOP>), groups_for(a.rows * sp.parts), dim3(LB), 0, s, a, sp.parts, sp.part);
     if (sp.parts > 1) hipLaunchKernelGGL((k_logp_join<T, ID, TOP>), dim3((unsigned)a.rows), dim3(LB), 0, s, a, sp.parts);
   }); }); });
 }
@@ -386,7 +393,7 @@ void launch_logp_grad(const LogpGradArgs& a, int dtype, int id_bits, hipStream_t
   with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) { with_flag(a.g_entropy != nullptr, [&](auto ent) {
     using T = decltype(t);
     const int64_t piece = 64 * 4 * Sixteen<T>::V, per_row = (a.vocab + piece - 1) / piece, pieces = a.rows * per_row, groups = (pieces + WAVES - 1) / WAVES;
-    hipLaunchKernelGGL((k_logp_grad<T, decltype(id), decltype(ent)::value>), dim3((unsigned)(groups < (1 << 24) ? groups : 1 << 24)), dim3(LB), 0, s, a, pieces, (int)per_row);
+    hipLaunchKernelGGL((k_logp_grad<T, decltype(id), decltype(ent)::value>), groups_for(groups), dim3(LB), 0, s, a, pieces, (int)per_row);
   }); }); });
 }
 

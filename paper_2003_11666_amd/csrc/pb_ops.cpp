@@ -1,6 +1,10 @@
 // C entries of the operators over plain device arrays (include/pb.h): arguments are checked here, before anything is launched.
 #include <math.h>
 
+#include <algorithm>
+#include <exception>
+#include <vector>
+
 #include "pb_ops.h"
 
 using namespace pb;
@@ -29,6 +33,30 @@ int bad_ids(const char* what, const void* ids, int id_bits) {
   return PB_OK;
 }
 
+// What a step writes must not overlap: a tensor that is listed twice would be updated twice at once.
+int disjoint(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_desc* d, int64_t blocks, void* m, void* v, uint8_t* m_exp, uint8_t* v_exp) {
+  struct Range { uintptr_t from, to; };
+  try {
+    std::vector<Range> r;
+    r.reserve(2 * (size_t)n_tensors + 4);
+    auto add = [&](const void* p, int64_t bytes) { if (p && bytes) r.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}); };
+    for (int32_t i = 0; i < n_tensors; ++i) {
+      add(ts[i].w, ts[i].n * (int64_t)size_of(d->w_type));
+      add(ts[i].w_hat, ts[i].n * (int64_t)size_of(d->w_hat_type));
+    }
+    add(m, blocks * PB_ADAMW_BLOCK * (d->moment_bits / 8));
+    add(v, blocks * PB_ADAMW_BLOCK * (d->moment_bits / 8));
+    add(m_exp, blocks);
+    add(v_exp, blocks);
+    std::sort(r.begin(), r.end(), [](const Range& x, const Range& y) { return x.from < y.from; });
+    for (size_t i = 1; i < r.size(); ++i)
+      if (r[i].from < r[i - 1].to) return fail(PB_E_INVALID, "weights, predicted weights and moments must not overlap");
+  } catch (const std::exception& e) {
+    return fail(PB_E_NOMEM, "out of host memory (%s)", e.what());
+  }
+  return PB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -47,7 +75,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   if (!d || n_tensors < 0 || (n_tensors > 0 && !ts)) return fail(PB_E_INVALID, "NULL argument");
   if (!is_type(d->w_type) || !is_type(d->g_type) || !is_type(d->w_hat_type)) return fail(PB_E_INVALID, "types must be PB_F32 or PB_BF16");
   if (d->moment_bits != 32 && d->moment_bits != 8) return fail(PB_E_INVALID, "moment_bits must be 32 or 8, not %d", (int)d->moment_bits);
-  if (!(d->lr >= 0) || !isfinite(d->lr) || !isfinite(d->horizon)) return fail(PB_E_INVALID, "lr must be >= 0, lr and horizon finite");
+  if (!(d->lr >= 0) || !isfinite((float)d->lr) || !isfinite((float)d->horizon)) return fail(PB_E_INVALID, "lr must be >= 0, lr and horizon finite");
   if (!(d->beta1 >= 0 && (float)d->beta1 < 1) || !(d->beta2 >= 0 && (float)d->beta2 < 1)) return fail(PB_E_INVALID, "betas must be in [0, 1)");
   if (!((float)d->eps > 0) || !isfinite(d->eps)) return fail(PB_E_INVALID, "eps must be positive (as a 32-bit number)");
   if (!d->step_dev && d->step < 1) return fail(PB_E_INVALID, "steps are counted from 1");
@@ -55,11 +83,11 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   int64_t blocks = 0, work = 0;
   for (int32_t i = 0; i < n_tensors; ++i) {
     const pb_adamw_tensor& t = ts[i];
-    if (t.n < 0 || t.n > MOST || (blocks += in_blocks(t.n)) > MOST / PB_ADAMW_BLOCK) return fail(PB_E_INVALID, "tensor %d: bad size", (int)i);
+    if (t.n < 0 || t.n > MOST_GROUPS * 4096 || (blocks += in_blocks(t.n)) > MOST / PB_ADAMW_BLOCK) return fail(PB_E_INVALID, "tensor %d: bad size", (int)i);
     if (t.n == 0) continue;
     ++work;
     if (!t.w || !t.g) return fail(PB_E_INVALID, "tensor %d: no weights or no gradient", (int)i);
-    if (!isfinite(t.weight_decay)) return fail(PB_E_INVALID, "tensor %d: weight_decay must be finite", (int)i);
+    if (!isfinite((float)(d->lr * t.weight_decay))) return fail(PB_E_INVALID, "tensor %d: lr * weight_decay must be finite", (int)i);
     if (!aligned(t.w, size_of(d->w_type)) || !aligned(t.g, size_of(d->g_type)) || !aligned(t.w_hat, size_of(d->w_hat_type)))
       return fail(PB_E_INVALID, "tensor %d: arrays must lie on boundaries of their element size", (int)i);
   }
@@ -67,6 +95,8 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   if (!m || !v || !aligned(m, 16) || !aligned(v, 16)) return fail(PB_E_INVALID, "m and v must be given, on 16-byte boundaries");
   if (d->moment_bits == 8 ? !m_exp || !v_exp : m_exp || v_exp)
     return fail(PB_E_INVALID, "m_exp and v_exp belong to 8-bit moments, and those to them");
+
+  if (const int rc = disjoint(ts, n_tensors, d, blocks, m, v, m_exp, v_exp)) return rc;
 
   AdamWArgs a = {};
   a.b1 = (float)d->beta1; a.c1 = (float)(1.0 - d->beta1);
@@ -93,8 +123,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
     const pb_adamw_tensor& t = ts[i];
     if (t.n == 0) continue;
     const int64_t g = (t.n + chunk - 1) / chunk;
-    if (g > 0x7fffffff) return fail(PB_E_INVALID, "tensor %d is too large", (int)i);
-    if (a.n_tensors == ADAMW_TENSORS || groups + g > 0x7fffffff) {
+    if (a.n_tensors == ADAMW_TENSORS || groups + g > MOST_GROUPS) {
       const int rc = launch();
       if (rc) return rc;
     }
@@ -112,7 +141,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
 }
 
 int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, void* stream) {
-  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST / 2) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
+  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST_GROUPS * 4096) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
   if (n == 0) return PB_OK;
   if (!m || !v || !m_exp || !v_exp || !m_out || !v_out) return fail(PB_E_INVALID, "NULL argument");
   if (((uintptr_t)m | (uintptr_t)v | (uintptr_t)m_out | (uintptr_t)v_out) % 16) return fail(PB_E_INVALID, "arrays must be 16-byte aligned");

@@ -13,6 +13,9 @@ namespace pb {
 
 int fail(int code, const char* fmt, ...);   // pb_host.cpp: the text of pb_last_error, returns code
 
+constexpr int64_t MAX_GROUPS = 1 << 20;   // workgroups of a launch that goes on in a loop
+constexpr int64_t MOST_GROUPS = (1 << 24) - 1;   // of 256 threads: a launch counts its threads in 32 bits
+
 // ------------------------------------------------------------------------------------------------ AdamW (pb_adamw.hip)
 constexpr int ADAMW_TENSORS = 64;    // tensors per launch: a lane each in the search for a workgroup's tensor, 3 KB of arguments
 // Elements per workgroup.  8-bit moments: a workgroup that goes on to more vectors has their requests under way while it

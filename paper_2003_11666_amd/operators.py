@@ -157,6 +157,8 @@ def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, w
             setattr(d, name, _type(ts[0], "adamw_step: tensors"))
     at = list(map(T.data_ptr, every))
     rec = np.zeros(n, dtype=_TENSOR)
+    if np.ndim(weight_decay) and np.shape(weight_decay) != (n,):
+        raise PBError("adamw_step: weight_decay must be a number, or one for each parameter")
     rec["w"], rec["g"], rec["n"], rec["weight_decay"] = at[:n], at[n:2 * n], sizes[:n], weight_decay
     if hats:
         rec["w_hat"] = at[2 * n:]
@@ -169,7 +171,7 @@ def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, w
             raise PBError(f"adamw_step: 8-bit moments, and only they, have exponents: uint8 of {total // ADAMW_BLOCK} elements")
     d.moment_bits = 8 if eight else 32
     d.lr, (d.beta1, d.beta2), d.eps, d.horizon = lr, betas, eps, horizon
-    d.step = 0 if step_dev is not None else int(step)
+    d.step = 0 if step_dev is not None else min(int(step), 2 ** 63 - 1)
     d.step_dev, d.grad_scale, d.seed = _ptr(step_dev), _ptr(grad_scale), int(seed) & 0xFFFFFFFFFFFFFFFF
     _call(index, lib.pb_adamw_step, rec.ctypes.data, n, C.byref(d), m.data_ptr(), v.data_ptr(), _ptr(m_exp), _ptr(v_exp))
 

@@ -143,6 +143,19 @@ def test_values_over_the_whole_range(bits):
         check(s, step=t, seed=t)
 
 
+def test_eight_bit_moments_from_zero_and_of_weights_without_gradients():
+    """Where training starts, and rows of a table that no token named: blocks of zeros beside others, and blocks that empty out."""
+    s = make((128 * 40, 700), bits=8, hat="float32")
+    for key in ("m", "v", "m_exp", "v_exp"):
+        s[key].zero_()
+    for t in range(1, 6):
+        g = s["g"][0].view(40, 128)
+        g.copy_(make((128 * 40,), seed=t)["w"][0].view(40, 128))
+        g[t::3] = 0
+        s["g"][1].mul_(-0.0 if t == 3 else 1.0)
+        check(s, step=t, seed=t, horizon=1.0)
+
+
 def test_eight_bit_second_moment_decays():
     """With gradients gone, v shrinks by beta2 a step on average though one step is far less than a code."""
     import torch
@@ -260,7 +273,7 @@ def test_refusals_of_tensors_on_the_gpu():
     from paper_2003_11666_amd import PBError, adamw_step
     w, m = torch.zeros(64, 4, device="cuda"), torch.zeros(256, device="cuda")
     for kw in (dict(params=[w.t()]), dict(grads=[w[:3]]), dict(m=m[:128]), dict(v=m.double()), dict(m=m.byte()), dict(m_exp=torch.zeros(2, dtype=torch.uint8, device="cuda")),
-               dict(params=[w.half()]), dict(params=[w, w.bfloat16()], grads=[w, w]), dict(grads=[w.cpu()]), dict(step=0), dict(betas=(1.0, 0.9)), dict(eps=0.0)):
+               dict(params=[w.half()]), dict(params=[w, w.bfloat16()], grads=[w, w]), dict(grads=[w.cpu()]), dict(weight_decay=[0.1, 0.2]), dict(predicted=[w]), dict(params=[w, w], grads=[w, w], m=m.new_zeros(512), v=m.new_zeros(512)), dict(step=0), dict(betas=(1.0, 0.9)), dict(eps=0.0)):
         a = {**dict(params=[w], grads=[w], m=m, v=m.clone(), step=1, lr=0.1), **kw}
         with pytest.raises(PBError):
             adamw_step(a.pop("params"), a.pop("grads"), a.pop("m"), a.pop("v"), **a)

@@ -310,6 +310,22 @@ def test_replayed_calls_are_the_eager_ones():
         check(x, t, top=16, got=r)
 
 
+def test_more_rows_than_a_launch_has_workgroups():
+    """2^24 + 5 rows of 3 logits: their rows repeat, and so must the results."""
+    import torch
+    from paper_2003_11666_amd import log_probs, log_probs_backward
+    n = (1 << 24) + 5
+    few = logits(1 << 12, 3, "bfloat16")
+    x, t = few.repeat(n // len(few) + 1, 1)[:n], targets(1 << 12, 3).repeat(n // len(few) + 1)[:n]
+    a, b = log_probs(x, t, top=1), log_probs(few, t[: len(few)], top=1)
+    g = torch.ones(n, device="cuda")
+    da, db = log_probs_backward(x, t, a.norm, g), log_probs_backward(few, t[: len(few)], b.norm, g[: len(few)])
+    for p, q in zip((*a, da), (*b, db)):
+        for at in range(0, n, 1 << 22):
+            part = p[at:at + (1 << 22)]
+            assert torch.equal(part, q.repeat(*([len(part) // len(q) + 1] + [1] * (q.dim() - 1)))[: len(part)]), at
+
+
 def test_a_row_beyond_32_bit_offsets():
     """Rows 2^30 bf16 elements apart: the third starts at 4 GiB."""
     import torch

@@ -181,3 +181,17 @@ def test_python_calls_refuse():
             call()
             print("accepted:", k)
     assert P.adamw_elements([f, torch.zeros(0), torch.zeros(129)]) == 128 + 256
+
+
+def test_adamw_refuses_what_it_would_write_twice():
+    """Weights, predicted weights and moments, each on its own 4096 bytes here, then two of them on the same."""
+    def rec(**kw):
+        r = np.zeros(2, dtype=P._TENSOR)
+        r["w"], r["w_hat"], r["g"], r["n"] = [A, A + 4096], [A + 8192, A + 12288], A, 1024
+        for k, x in kw.items():
+            r[k] = x
+        return r
+    m, v = A + 16384, A + 16384 + 2 * 4096
+    for r, m_, v_ in ((rec(w=A), m, v), (rec(w=[A, A + 4092]), m, v), (rec(w_hat=[A, A + 12288]), m, v), (rec(), A, v), (rec(), m, m + 8188 // 16 * 16),
+                      (rec(), A + 12288 + 4080, v)):
+        refused(step(rec=r, m=m_, v=v_), "overlap")
