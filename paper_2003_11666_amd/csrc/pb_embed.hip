@@ -6,60 +6,74 @@ namespace pb {
 constexpr int EB = 256;   // threads per workgroup
 constexpr int EW = EB / 64;
 
-// V columns of a row as floats, from column j on, of which `have` exist.
-template <class T, int V> __device__ __forceinline__ void read_columns(float (&f)[V], const T* p, int have) {
-  if (have >= V) {
-#pragma unroll
-    for (int i = 0; i < V; i += Sixteen<T>::V) {
-      Sixteen<T> q;
-      q.load(p + i);
-#pragma unroll
-      for (int e = 0; e < Sixteen<T>::V; ++e) f[i + e] = q.get(e);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = e < have ? to_float(p[e]) : 0.f;
-  }
-}
-template <class T, int V> __device__ __forceinline__ void write_columns(T* p, const float (&f)[V], int have) {
-  if (have >= V) {
-#pragma unroll
-    for (int i = 0; i < V; i += Sixteen<T>::V) {
-      Sixteen<T> q;
-      float part[Sixteen<T>::V];
-#pragma unroll
-      for (int e = 0; e < Sixteen<T>::V; ++e) part[e] = f[i + e];
-      q.put(part);
-      q.store(p + i);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < have) p[e] = from_float<T>(f[e]);
-  }
-}
-
 constexpr int EV = 8;              // columns of a lane: 16 bytes of bf16
 constexpr int SLICE = 64 * EV;     // of a wavefront
+
+// A lane's columns of the slice that starts at column j0.  Where a slice has EV of them at least, all lanes have EV, the last ones
+// those that end the row: some of these are another lane's as well, who reads, computes and writes the same.  (No lane takes a
+// way of its own, so that requests stay under way together.)  Else the first lane has what there is, an element at a time.
+struct Lane { int64_t j; int have; bool whole, active; };
+__device__ __forceinline__ Lane columns(int64_t j0, int64_t dim) {
+  const int lane = threadIdx.x & 63;
+  const int64_t j = j0 + lane * EV;
+  if (dim - j0 >= EV) return {j < dim - EV ? j : dim - EV, EV, true, j < dim};
+  return {j0, lane == 0 ? (int)(dim - j0) : 0, false, lane == 0};
+}
+
+// EV columns as they lie in memory.
+template <class T> struct Columns {
+  static constexpr int N = EV / Sixteen<T>::V;
+  Sixteen<T> q[N];
+  template <bool ONCE = false> __device__ __forceinline__ void load(const T* p, const Lane& l) {
+    if (l.whole) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) q[i].template load<ONCE>(p + i * Sixteen<T>::V);
+    } else {
+      float f[EV];
+#pragma unroll
+      for (int e = 0; e < EV; ++e) f[e] = to_float(p[e < l.have ? e : 0]);
+      put(f);
+    }
+  }
+  __device__ __forceinline__ void store(T* p, const Lane& l) const {
+    if (!l.active) return;
+    if (l.whole) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) q[i].store(p + i * Sixteen<T>::V);
+    } else {
+#pragma unroll
+      for (int e = 0; e < EV; ++e)
+        if (e < l.have) p[e] = from_float<T>(get(e));
+    }
+  }
+  __device__ __forceinline__ float get(int e) const { return q[e / Sixteen<T>::V].get(e % Sixteen<T>::V); }
+  __device__ __forceinline__ void put(const float (&f)[EV]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float part[Sixteen<T>::V];
+#pragma unroll
+      for (int e = 0; e < Sixteen<T>::V; ++e) part[e] = f[i * Sixteen<T>::V + e];
+      q[i].put(part);
+    }
+  }
+};
 
 // ------------------------------------------------------------------------------------------------------------- lookup
 // Bound by memory.  A wavefront takes SLICE columns of one token.
 template <class T, class O, class ID>
 __global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a, int64_t pieces, int slices) {
-  const int lane = threadIdx.x & 63;
   for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces; p += (int64_t)gridDim.x * EW) {
-    const int64_t i = p / slices, j = (p - i * slices) * SLICE + lane * EV, id = ((const ID*)a.ids)[i];
-    const int64_t have = a.dim - j;
-    if (have <= 0) continue;
-    float f[EV] = {};
-    if (id >= 0 && id < a.vocab) read_columns<T, EV>(f, (const T*)a.table + id * a.dim + j, have < EV ? (int)have : EV);
+    const int64_t i = p / slices, id = ((const ID*)a.ids)[i];
+    const Lane l = columns((p - i * slices) * SLICE, a.dim);
+    const bool there = id >= 0 && id < a.vocab;
+    Columns<T> row;
+    row.load((const T*)a.table + (there ? id : 0) * a.dim + l.j, l);
+    float f[EV];
 #pragma unroll
-    for (int e = 0; e < EV; ++e) f[e] *= a.scale;
-    if (!(id >= 0 && id < a.vocab)) {
-#pragma unroll
-      for (int e = 0; e < EV; ++e) f[e] = 0.f;
-    }
-    write_columns<O, EV>((O*)a.out + i * a.dim + j, f, have < EV ? (int)have : EV);
+    for (int e = 0; e < EV; ++e) f[e] = there ? row.get(e) * a.scale : 0.f;
+    Columns<O> out;
+    out.put(f);
+    out.store((O*)a.out + i * a.dim + l.j, l);
   }
 }
 
@@ -283,41 +297,20 @@ k_scatter(const void* in, const uint32_t* place_in, int64_t n, int64_t vocab, in
 // each row of gradients is read once, in whole cache lines.
 struct Sorted { const uint32_t *key, *place; int64_t n; int chunk; float* part; };   // part [chunk][2][dim]
 
-// EV columns as they lie in memory.
-template <class T> struct Columns {
-  Sixteen<T> q[EV / Sixteen<T>::V];
-  template <bool ONCE = false> __device__ __forceinline__ void load(const T* p, int have) {
-    if (have == EV) {
-#pragma unroll
-      for (int i = 0; i < EV / Sixteen<T>::V; ++i) q[i].template load<ONCE>(p + i * Sixteen<T>::V);
-    } else {
-      float f[EV];
-      read_columns<T, EV>(f, p, have);
-#pragma unroll
-      for (int i = 0; i < EV / Sixteen<T>::V; ++i) {
-        float part[Sixteen<T>::V];
-#pragma unroll
-        for (int e = 0; e < Sixteen<T>::V; ++e) part[e] = f[i * Sixteen<T>::V + e];
-        q[i].put(part);
-      }
-    }
-  }
-  __device__ __forceinline__ float get(int e) const { return q[e / Sixteen<T>::V].get(e % Sixteen<T>::V); }
-};
-
 // was: the row before (ADD)
 template <class O, bool ADD>
-__device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t id, int64_t j, float (&s)[EV], const Columns<O>& was, int have) {
+__device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t id, const Lane& l, float (&s)[EV], const Columns<O>& was) {
 #pragma unroll
   for (int e = 0; e < EV; ++e) s[e] = ADD ? was.get(e) + s[e] * a.scale : s[e] * a.scale;
-  write_columns<O, EV>((O*)a.d_table + id * a.dim + j, s, have);
+  Columns<O> row;
+  row.put(s);
+  row.store((O*)a.d_table + id * a.dim + l.j, l);
 }
 
 template <class T, class O, bool ADD>
-__device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& s, int64_t c, int64_t j) {
+__device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& s, int64_t c, const Lane& l) {
   constexpr int B = ADD ? 4 : 8;   // rows under way, with ADD the rows of the table that they end in as well
   const int lane = threadIdx.x & 63;
-  const int have = a.dim - j >= EV ? EV : a.dim > j ? (int)(a.dim - j) : 0;
   const int64_t lo = c * s.chunk, hi = lo + s.chunk < s.n ? lo + s.chunk : s.n;
   const uint32_t first = s.key[lo], ahead = lo > 0 ? s.key[lo - 1] : 0xFFFFFFFFu;
   bool began_before = first == ahead;
@@ -333,8 +326,8 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& 
       for (int b = 0; b < B; ++b) {
         const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)key, b0 + b), at = (uint32_t)__builtin_amdgcn_readlane((int)place, b0 + b);
         if (id >= (uint64_t)a.vocab) continue;
-        row[b].template load<true>((const T*)a.d_out + (int64_t)at * a.dim + j, have);
-        if (ADD && (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id) was[b].load((const O*)a.d_table + (int64_t)id * a.dim + j, have);
+        row[b].template load<true>((const T*)a.d_out + (int64_t)at * a.dim + l.j, l);
+        if (ADD && (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id) was[b].load((const O*)a.d_table + (int64_t)id * a.dim + l.j, l);
       }
 #pragma unroll
       for (int b = 0; b < B; ++b) {
@@ -344,8 +337,12 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& 
         for (int e = 0; e < EV; ++e) acc[e] += row[b].get(e);
         const bool ends = (uint32_t)__builtin_amdgcn_readlane((int)next, b0 + b) != id;
         if (!ends && k0 + b0 + b + 1 < hi) continue;
-        if (ends && !began_before) put_row<O, ADD>(a, id, j, acc, was[ADD ? b : 0], have);
-        else write_columns<float, EV>(s.part + (2 * c + (began_before ? 0 : 1)) * a.dim + j, acc, have);
+        if (ends && !began_before) put_row<O, ADD>(a, id, l, acc, was[ADD ? b : 0]);
+        else {
+          Columns<float> part;
+          part.put(acc);
+          part.store(s.part + (2 * c + (began_before ? 0 : 1)) * a.dim + l.j, l);
+        }
 #pragma unroll
         for (int e = 0; e < EV; ++e) acc[e] = 0.f;
         began_before = false;
@@ -354,11 +351,13 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& 
   }
 }
 
-// Rows of the table that no token names, 64 to a wavefront: each lane looks its own up among the sorted ids.
-constexpr int EMPTY_ROWS = 64;
-template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArgs& a, const Sorted& s, int64_t r0) {
+// Rows of the table that no token names, `rows` to a wavefront: a lane looks up one of them among the sorted ids.  64 beside many
+// sums (131072 tokens: 102 us, 110 with 16, whose searches take their places), 16 where there is little else to do (259
+// tokens: 58 MB of zeros in 19 us, 24 with 64).
+int rows_to_clear(int64_t pieces) { return pieces < 4096 ? 16 : 64; }
+template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArgs& a, const Sorted& s, int64_t r0, int rows) {
   const int lane = threadIdx.x & 63;
-  const int64_t r = r0 + lane;
+  const int64_t r = lane < rows ? r0 + lane : a.vocab;
   int64_t lo = 0, hi = s.n;   // the first sorted token of an id >= r
   while (__any(lo < hi)) {
     const int64_t mid = (lo + hi) >> 1;
@@ -369,26 +368,33 @@ template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArg
   }
   const bool empty = r < a.vocab && !(lo < s.n && (int64_t)s.key[lo] == r);
   const float zero[EV] = {};
+  Columns<O> zeros;
+  zeros.put(zero);
   for (uint64_t more = __ballot(empty); more; more &= more - 1) {
     O* out = (O*)a.d_table + (r0 + __builtin_ctzll(more)) * a.dim;
-    for (int64_t j = lane * EV; j < a.dim; j += SLICE) write_columns<O, EV>(out + j, zero, a.dim - j < EV ? (int)(a.dim - j) : EV);
+    for (int64_t j0 = 0; j0 < a.dim; j0 += SLICE) {
+      const Lane l = columns(j0, a.dim);
+      zeros.store(out + l.j, l);
+    }
   }
 }
 
 template <class T, class O, bool ADD>
-__global__ void __launch_bounds__(EB) k_sums(const EmbedGradArgs a, const Sorted s, int64_t pieces, int slices, int64_t clears) {
+__global__ void __launch_bounds__(EB) k_sums(const EmbedGradArgs a, const Sorted s, int64_t pieces, int slices, int64_t clears, int rows) {
   for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces + clears; p += (int64_t)gridDim.x * EW) {
     const int64_t q = p - clears;   // (rows to clear first: their searches wait for one load after the other)
-    if (q < 0) clear_rows<O>(a, s, p * EMPTY_ROWS);
-    else sum_chunk<T, O, ADD>(a, s, q / slices, (q % slices) * SLICE + (threadIdx.x & 63) * EV);
+    if (q < 0) clear_rows<O>(a, s, p * rows, rows);
+    else sum_chunk<T, O, ADD>(a, s, q / slices, columns((q % slices) * SLICE, a.dim));
   }
 }
 
 // The id that starts in a chunk and goes on beyond it: its part of the chunk and those of the chunks behind, dealt out to the
-// wavefronts of a workgroup.
+// wavefronts of a workgroup, which have eight of them under way each: an id that a fifth
+// of 46266 tokens share has 200 parts (11 us; 20 with the requests one behind the other).
+constexpr int JB = 256, JW = JB / 64, JOINED = 8;
 template <class O, bool ADD>
-__global__ void __launch_bounds__(EB) k_join(const EmbedGradArgs a, const Sorted s, int64_t chunks) {
-  __shared__ float sums[EW][SLICE];
+__global__ void __launch_bounds__(JB) k_join(const EmbedGradArgs a, const Sorted s, int64_t chunks) {
+  __shared__ float sums[JW][SLICE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = blockIdx.x, lo = c * s.chunk, hi = lo + s.chunk;
   if (hi >= s.n) return;
@@ -402,26 +408,36 @@ __global__ void __launch_bounds__(EB) k_join(const EmbedGradArgs a, const Sorted
     if (on != ~0ull) break;
   }
   for (int64_t j0 = (int64_t)blockIdx.y * SLICE; j0 < a.dim; j0 += (int64_t)gridDim.y * SLICE) {
-    const int64_t j = j0 + lane * EV;
-    const int have = a.dim - j >= EV ? EV : a.dim > j ? (int)(a.dim - j) : 0;
+    const Lane l = columns(j0, a.dim);
     float acc[EV] = {};
     Columns<O> was;
-    if (ADD && wave == 0) was.load((const O*)a.d_table + (int64_t)id * a.dim + j, have);
-#pragma unroll 4
-    for (int64_t k = wave; k <= behind; k += EW) {
-      float f[EV];
-      read_columns<float, EV>(f, s.part + (2 * (c + k) + (k == 0)) * a.dim + j, have);
+    if (ADD && wave == 0) was.load((const O*)a.d_table + (int64_t)id * a.dim + l.j, l);
+    auto parts = [&](const Lane& l) {
+      for (int64_t k0 = wave; k0 <= behind; k0 += JOINED * JW) {
+        Columns<float> q[JOINED];
 #pragma unroll
-      for (int e = 0; e < EV; ++e) acc[e] += f[e];
-    }
+        for (int i = 0; i < JOINED; ++i) {
+          const int64_t k = k0 + i * JW < behind ? k0 + i * JW : behind;   // (beyond the last: read again, not added)
+          q[i].load(s.part + (2 * (c + k) + (k == 0)) * a.dim + l.j, l);
+        }
+#pragma unroll
+        for (int i = 0; i < JOINED; ++i) {
+          const bool counts = k0 + i * JW <= behind;   // (no branch: the requests would move behind it)
+#pragma unroll
+          for (int e = 0; e < EV; ++e) acc[e] += counts ? q[i].get(e) : 0.f;
+        }
+      }
+    };
+    if (l.whole) parts(Lane{l.j, EV, true, l.active});   // (a copy for each, so that neither carries the other's registers)
+    else parts(Lane{l.j, l.have, false, l.active});
 #pragma unroll
     for (int e = 0; e < EV; ++e) sums[wave][e * 64 + lane] = acc[e];
     __syncthreads();
     if (wave == 0) {
-      for (int w = 1; w < EW; ++w)
+      for (int w = 1; w < JW && w <= behind; ++w)
 #pragma unroll
         for (int e = 0; e < EV; ++e) acc[e] += sums[w][e * 64 + lane];
-      put_row<O, ADD>(a, id, j, acc, was, have);
+      put_row<O, ADD>(a, id, l, acc, was);
     }
     __syncthreads();
   }
@@ -437,8 +453,12 @@ dim3 groups_for(int64_t wavefronts) {
 
 int64_t in_slices(int64_t dim) { return (dim + SLICE - 1) / SLICE; }
 
-// Tokens per chunk: 2048 chunks at most, so that few parts are left of an id that most tokens share, and 8 tokens at least.
-int chunk_of(int64_t n) { return (int)(n / 2048 < 8 ? 8 : (n + 2047) / 2048); }
+// Tokens per chunk: 8 at least, and so many that about 4096 wavefronts share the sums, in 512 to 2048 chunks: an id that most
+// tokens share leaves a part in each of them.
+int chunk_of(int64_t n, int64_t dim) {
+  const int64_t want = 4096 / in_slices(dim), chunks = want < 512 ? 512 : want > 2048 ? 2048 : want, chunk = (n + chunks - 1) / chunks;
+  return (int)(chunk < 8 ? 8 : chunk);
+}
 
 struct Layout { int64_t key[2], place[2], counts, total, part, bytes, tiles; };
 Layout layout(int64_t n, int64_t dim) {
@@ -454,7 +474,7 @@ Layout layout(int64_t n, int64_t dim) {
     l.counts = take(4 * BINS * l.tiles);
     l.total = take(4 * BINS);
   }
-  const int64_t chunk = chunk_of(n), chunks = (n + chunk - 1) / chunk;
+  const int64_t chunk = chunk_of(n, dim), chunks = (n + chunk - 1) / chunk;
   l.part = take(8 * chunks * dim);
   return l;
 }
@@ -496,14 +516,14 @@ void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int i
         hipLaunchKernelGGL((k_scatter<ID, false>), grid, dim3(EB), 0, s, key, place, a.n, a.vocab, p * width, width, l.tiles, at(l.counts), at(l.total), key_to, place_to);
     }
   });
-  const int chunk = chunk_of(a.n);
-  const int64_t chunks = (a.n + chunk - 1) / chunk, slices = in_slices(a.dim), clears = a.add ? 0 : (a.vocab + EMPTY_ROWS - 1) / EMPTY_ROWS;
+  const int chunk = chunk_of(a.n, a.dim);
+  const int64_t chunks = (a.n + chunk - 1) / chunk, slices = in_slices(a.dim), rows = rows_to_clear(chunks * slices), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
   const Sorted sorted = {at(l.key[from]), at(l.place[from]), a.n, chunk, (float*)at(l.part)};
   with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) { with_flag(a.add != 0, [&](auto add) {
     constexpr bool ADD = decltype(add)::value;
-    hipLaunchKernelGGL((k_sums<decltype(t), decltype(o), ADD>), groups_for(chunks * slices + clears), dim3(EB), 0, s, a, sorted, chunks * slices, (int)slices, clears);
+    hipLaunchKernelGGL((k_sums<decltype(t), decltype(o), ADD>), groups_for(chunks * slices + clears), dim3(EB), 0, s, a, sorted, chunks * slices, (int)slices, clears, (int)rows);
     if (chunks > 1)
-      hipLaunchKernelGGL((k_join<decltype(o), ADD>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(EB), 0, s, a, sorted, chunks);
+      hipLaunchKernelGGL((k_join<decltype(o), ADD>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(JB), 0, s, a, sorted, chunks);
   }); }); });
 }
 

@@ -154,6 +154,8 @@ template <class T, bool TOP>
 __device__ __forceinline__ void scan(const T* x, uint32_t lo, uint32_t hi, uint32_t wave, uint32_t waves, float scale, Sums& a, Best& best) {
   constexpr uint32_t V = Sixteen<T>::V, U = 4;   // four requests of a lane under way
   const uint32_t lane = threadIdx.x & 63, whole = lo + (hi - lo) / V * V;
+  const uint32_t last = whole + lane < hi ? whole + lane : lo;   // (what no vector holds, requested before all else)
+  const T rest = x[last];
   bool first = true;
   for (uint32_t j0 = lo + (wave * 64 + lane) * V; j0 - lane * V < whole; j0 += U * waves * 64 * V) {
     Sixteen<T> q[U];
@@ -194,7 +196,7 @@ __device__ __forceinline__ void scan(const T* x, uint32_t lo, uint32_t hi, uint3
   }
   if (whole < hi && wave == 0) {   // what no vector holds
     const bool mine = whole + lane < hi;
-    const float z = mine ? to_float(x[whole + lane]) : -INFINITY;
+    const float z = mine ? to_float(rest) : -INFINITY;
     const float y[1] = {z * scale};
     take(a, y);
     if (TOP) best.enter(mine ? top_key(z, whole + lane) : 0);
@@ -322,13 +324,19 @@ __global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t 
   const int lane = threadIdx.x & 63;
   for (int64_t p = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); p < pieces; p += (int64_t)gridDim.x * WAVES) {
     const int64_t r = p / per_row;
-    const uint32_t vocab = (uint32_t)a.vocab, j0 = (uint32_t)(p - r * per_row) * PIECE + lane * V;
+    const uint32_t vocab = (uint32_t)a.vocab, p0 = (uint32_t)(p - r * per_row) * PIECE;
     const T* x = (const T*)a.logits + r * a.stride;
     T* d = (T*)a.d + r * a.d_stride;
+    // (a lane whose vector would pass the row's end takes the row's last one: some of it is another lane's as well, who computes
+    // the same.  The wavefront has read all of its piece before it writes, for gradients in place of the logits.)
+    const bool whole = vocab - p0 >= V;
+    uint32_t at[U];
     Sixteen<T> q[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (j0 + (i * 64 + 1) * V <= vocab) q[i].template load<true>(x + j0 + i * 64 * V);
+    for (int i = 0; i < U; ++i) {
+      at[i] = p0 + (i * 64 + lane) * V;
+      if (whole && p0 + i * 64 * V < vocab) q[i].template load<true>(x + (at[i] < vocab - V ? at[i] : vocab - V));
+    }
     const float m = a.norm[2 * r], ls = a.norm[2 * r + 1], ref = against(m);
     const int64_t t = a.g_logp ? (int64_t)((const ID*)a.targets)[r] : -1;
     const float gl = t >= 0 && t < vocab ? a.g_logp[r] : 0.f;
@@ -340,18 +348,19 @@ __global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t 
       if (ENT) y = fmaf(ge, fmaxf(ln, -150.f) + h, gl);
       return m == -INFINITY ? 0.f : ((j == t ? gl : 0.f) - p * y) * scale;
     };
+    if (!whole) {   // less than a vector: an element to a lane
+      if (p0 + lane < vocab) d[p0 + lane] = from_float<T>(grad(to_float(x[p0 + lane]), p0 + lane));
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const uint32_t j = j0 + i * 64 * V;
-      if (j + V <= vocab) {
-        float y[V];
+      if (at[i] >= vocab) continue;
+      const uint32_t j = at[i] < vocab - V ? at[i] : vocab - V;
+      float y[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = grad(q[i].get(e), j + e);
-        q[i].put(y);
-        q[i].template store<true>(d + j);
-      } else {
-        for (uint32_t e = j; e < vocab; ++e) d[e] = from_float<T>(grad(to_float(x[e]), e));
-      }
+      for (int e = 0; e < V; ++e) y[e] = grad(q[i].get(e), j + e);
+      q[i].put(y);
+      q[i].template store<true>(d + j);
     }
   }
 }
