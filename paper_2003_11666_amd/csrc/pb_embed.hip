@@ -351,6 +351,20 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& 
   }
 }
 
+// Zeros into those of the rows r0, r0 + 1, ... of the table whose lane says so.
+template <class O> __device__ __forceinline__ void clear(const EmbedGradArgs& a, int64_t r0, bool empty) {
+  const float zero[EV] = {};
+  Columns<O> zeros;
+  zeros.put(zero);
+  for (uint64_t more = __ballot(empty); more; more &= more - 1) {
+    O* out = (O*)a.d_table + (r0 + __builtin_ctzll(more)) * a.dim;
+    for (int64_t j0 = 0; j0 < a.dim; j0 += SLICE) {
+      const Lane l = columns(j0, a.dim);
+      zeros.store(out + l.j, l);
+    }
+  }
+}
+
 // Rows of the table that no token names, `rows` to a wavefront: a lane looks up one of them among the sorted ids.  64 beside many
 // sums (131072 tokens: 102 us, 110 with 16, whose searches take their places), 16 where there is little else to do (259
 // tokens: 58 MB of zeros in 19 us, 24 with 64).
@@ -366,17 +380,7 @@ template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArg
       else hi = mid;
     }
   }
-  const bool empty = r < a.vocab && !(lo < s.n && (int64_t)s.key[lo] == r);
-  const float zero[EV] = {};
-  Columns<O> zeros;
-  zeros.put(zero);
-  for (uint64_t more = __ballot(empty); more; more &= more - 1) {
-    O* out = (O*)a.d_table + (r0 + __builtin_ctzll(more)) * a.dim;
-    for (int64_t j0 = 0; j0 < a.dim; j0 += SLICE) {
-      const Lane l = columns(j0, a.dim);
-      zeros.store(out + l.j, l);
-    }
-  }
+  clear<O>(a, r0, r < a.vocab && !(lo < s.n && (int64_t)s.key[lo] == r));
 }
 
 template <class T, class O, bool ADD>
@@ -443,6 +447,60 @@ __global__ void __launch_bounds__(JB) k_join(const EmbedGradArgs a, const Sorted
   }
 }
 
+// ---------------------------------------------------------------------------------------------------------- a few tokens
+// One launch and no workspace: a wavefront for each token and slice, which holds the ids of all.  The first token of an id adds
+// up its rows, the others have nothing to do.  Up to 128 tokens, since one wavefront has all the rows of an id.
+constexpr int HANDFUL = 128;
+template <class T, class O, class ID, bool ADD>
+__global__ void __launch_bounds__(EB) k_handful(const EmbedGradArgs a, int slices, int64_t pieces, int64_t clears, int rows) {
+  constexpr int R = HANDFUL / 64, B = 8;
+  const int lane = threadIdx.x & 63, n = (int)a.n;
+  uint32_t key[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) key[r] = r * 64 + lane < n ? id_key(((const ID*)a.ids)[r * 64 + lane], a.vocab) : (uint32_t)a.vocab;
+  for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces + clears; p += (int64_t)gridDim.x * EW) {
+    if (p >= pieces) {
+      const int64_t r0 = (p - pieces) * rows;
+      bool empty = lane < rows && r0 + lane < a.vocab;
+      for (int i = 0; i < n; ++i)
+        if ((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(i < 64 ? key[0] : key[R - 1]), i & 63) == r0 + lane) empty = false;
+      clear<O>(a, r0, empty);
+      continue;
+    }
+    const int i = (int)(p / slices);
+    const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)(i < 64 ? key[0] : key[R - 1]), i & 63);
+    if (id >= (uint64_t)a.vocab) continue;
+    uint64_t who[R] = {__ballot(key[0] == id), __ballot(key[R - 1] == id)};
+    if (i != (who[0] ? __builtin_ctzll(who[0]) : 64 + __builtin_ctzll(who[1]))) continue;
+    const Lane l = columns((p % slices) * SLICE, a.dim);
+    Columns<O> was;
+    if (ADD) was.load((const O*)a.d_table + (int64_t)id * a.dim + l.j, l);
+    float acc[EV] = {};
+    while (who[0] | who[1]) {
+      Columns<T> row[B];
+      bool counts[B];
+      int at = i;
+#pragma unroll
+      for (int b = 0; b < B; ++b) {   // (beyond the last: the last again, not added)
+        counts[b] = (who[0] | who[1]) != 0;
+        if (counts[b]) {
+          const int h = who[0] ? 0 : 1;
+          at = h * 64 + __builtin_ctzll(h ? who[1] : who[0]);
+          if (h) who[1] &= who[1] - 1;
+          else who[0] &= who[0] - 1;
+        }
+        row[b].load((const T*)a.d_out + (int64_t)at * a.dim + l.j, l);
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int e = 0; e < EV; ++e) acc[e] += counts[b] ? row[b].get(e) : 0.f;
+    }
+    put_row<O, ADD>(a, id, l, acc, was);
+  }
+}
+static_assert(HANDFUL == 128, "two registers of ids");
+
 // ------------------------------------------------------------------------------------------------------------ launches
 namespace {
 
@@ -488,9 +546,17 @@ void launch_embed(const EmbedArgs& a, int dtype, int out_dtype, int id_bits, hip
   }); }); });
 }
 
-int64_t embed_grad_workspace(int64_t n, int64_t, int64_t dim) { return n > 0 ? layout(n, dim).bytes : 0; }
+int64_t embed_grad_workspace(int64_t n, int64_t, int64_t dim) { return n > HANDFUL ? layout(n, dim).bytes : 0; }
 
 void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int id_bits, hipStream_t s) {
+  const int64_t slices = in_slices(a.dim);
+  if (a.n <= HANDFUL) {
+    const int64_t pieces = a.n * slices, rows = rows_to_clear(pieces), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
+    with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) { with_id(id_bits, [&](auto id) { with_flag(a.add != 0, [&](auto add) {
+      hipLaunchKernelGGL((k_handful<decltype(t), decltype(o), decltype(id), decltype(add)::value>), groups_for(pieces + clears), dim3(EB), 0, s, a, (int)slices, pieces, clears, (int)rows);
+    }); }); }); });
+    return;
+  }
   char* ws = (char*)a.workspace;
   const Layout l = layout(a.n, a.dim);
   auto at = [&](int64_t o) { return (uint32_t*)(ws + o); };
@@ -498,7 +564,7 @@ void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int i
   while (a.vocab >> bits) ++bits;
   const int passes = (bits + DIGIT - 1) / DIGIT, width = (bits + passes - 1) / passes;
   int from = 0;
-  if (a.n > 0) with_id(id_bits, [&](auto id) {
+  with_id(id_bits, [&](auto id) {
     using ID = decltype(id);
     if (a.n <= FEW) {
       hipLaunchKernelGGL((k_rank<ID>), dim3((unsigned)((a.n + RANKED - 1) / RANKED)), dim3(RB), 0, s, (const ID*)a.ids, (int)a.n, a.vocab, at(l.key[0]), at(l.place[0]));
@@ -517,13 +583,12 @@ void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int i
     }
   });
   const int chunk = chunk_of(a.n, a.dim);
-  const int64_t chunks = (a.n + chunk - 1) / chunk, slices = in_slices(a.dim), rows = rows_to_clear(chunks * slices), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
+  const int64_t chunks = (a.n + chunk - 1) / chunk, rows = rows_to_clear(chunks * slices), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
   const Sorted sorted = {at(l.key[from]), at(l.place[from]), a.n, chunk, (float*)at(l.part)};
   with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) { with_flag(a.add != 0, [&](auto add) {
     constexpr bool ADD = decltype(add)::value;
     hipLaunchKernelGGL((k_sums<decltype(t), decltype(o), ADD>), groups_for(chunks * slices + clears), dim3(EB), 0, s, a, sorted, chunks * slices, (int)slices, clears, (int)rows);
-    if (chunks > 1)
-      hipLaunchKernelGGL((k_join<decltype(o), ADD>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(JB), 0, s, a, sorted, chunks);
+    hipLaunchKernelGGL((k_join<decltype(o), ADD>), dim3((unsigned)chunks, (unsigned)(slices < 64 ? slices : 64)), dim3(JB), 0, s, a, sorted, chunks);
   }); }); });
 }
 

@@ -234,7 +234,7 @@ def log_probs(logits, targets=None, *, scale=1.0, top=0, entropy=True):
     bits = _targets(targets, lead, "log_probs")
     top = int(top)
     need = _check(lib, lib.pb_log_probs_workspace(rows, vocab, top))
-    new = lambda shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+    new = lambda shape, dtype=torch.float32: logits.new_empty(shape, dtype=dtype)  # noqa: E731
     r = LogProbs(new(lead) if targets is not None else None, new(lead) if entropy else None, new((*lead, 2)),
                  new((*lead, top)) if top else None, new((*lead, top), torch.int64 if bits == 64 else torch.int32) if top else None)
     ws = new(need, torch.uint8) if need else None
@@ -256,7 +256,7 @@ def log_probs_backward(logits, targets, norm, g_logp, *, entropy=None, g_entropy
     _floats("log_probs_backward: norm", (*lead, 2), norm)
     _floats("log_probs_backward: entropy, g_logp and g_entropy", lead, entropy, g_logp, g_entropy)
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = logits.new_empty(logits.shape)
     if out.dtype != logits.dtype or out.shape != logits.shape:
         raise PBError("log_probs_backward: out must have the logits' shape and type")
     index = _on_gpu("log_probs_backward", logits, targets, norm, g_logp, entropy, g_entropy, out)
@@ -281,7 +281,7 @@ def embed(table, ids, *, scale=1.0, dtype=None):
     vocab, dim = _table(table, "embed")
     _dense("embed", ids)
     index = _on_gpu("embed", table, ids)
-    out = torch.empty((*ids.shape, dim), dtype=dtype or table.dtype, device=table.device)
+    out = table.new_empty((*ids.shape, dim), dtype=dtype or table.dtype)
     _call(index, lib.pb_embed, table.data_ptr(), kind, vocab, dim, ids.data_ptr(), bits, ids.numel(), scale, out.data_ptr(), _type(out, "embed: out"))
     return out
 
@@ -297,7 +297,7 @@ def embed_backward(d_out, ids, d_table, *, scale=1.0, add=False):
     _dense("embed_backward", d_out, ids)
     index = _on_gpu("embed_backward", d_out, ids, d_table)
     need = _check(lib, lib.pb_embed_backward_workspace(ids.numel(), vocab, dim))
-    ws = torch.empty(need, dtype=torch.uint8, device=d_table.device) if need else None
+    ws = d_table.new_empty(need, dtype=torch.uint8) if need else None
     _call(index, lib.pb_embed_backward, d_out.data_ptr(), kind, ids.data_ptr(), bits, ids.numel(), vocab, dim, scale, d_table.data_ptr(),
           _type(d_table, "embed_backward: d_table"), int(bool(add)), _ptr(ws), need)
     return d_table

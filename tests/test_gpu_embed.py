@@ -68,7 +68,7 @@ def check_grad(g, ids, start, *, scale=0.7, add=True, call=None):
 
 @pytest.mark.parametrize("add", [True, False])
 @pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "none", "rising", "falling"])
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 1000, 4097, 20000, 70001])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 127, 128, 129, 1000, 4097, 8192, 8193, 20000, 70001])
 def test_gradient(n, kind, add):
     g = table(n, 24, "float32", seed=n)
     for vocab in (1, 2, 300, 70000):

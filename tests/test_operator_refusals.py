@@ -143,7 +143,7 @@ def test_embed_refuses(kw, text):
     (dict(ws=A + 8), "workspace"),
 ])
 def test_embed_backward_refuses(kw, text):
-    a = {**dict(d_out=A, dtype=0, ids=A, id_bits=64, n=3, vocab=10, dim=4, scale=1.0, d_table=A, table_dtype=0, add=0, ws=A, ws_bytes=1 << 40), **kw}
+    a = {**dict(d_out=A, dtype=0, ids=A, id_bits=64, n=3000, vocab=10, dim=4, scale=1.0, d_table=A, table_dtype=0, add=0, ws=A, ws_bytes=1 << 40), **kw}
     refused(lib().pb_embed_backward(a["d_out"], a["dtype"], a["ids"], a["id_bits"], a["n"], a["vocab"], a["dim"], a["scale"], a["d_table"],
                                     a["table_dtype"], a["add"], a["ws"], a["ws_bytes"], None), text)
 
