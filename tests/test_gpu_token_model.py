@@ -59,3 +59,33 @@ def test_training_steps_of_a_tied_model(bits):
                 (w2, *_), (bw, *_) = R.adamw(w0, R.f64(grad).ravel(), zero, zero, step=1, lr=0.01, b1=0.9, b2=0.999, eps=1e-8, decay=wd, horizon=0, w_half=R.EPS, hat_half=0)
                 assert np.all(np.abs(R.f64(t).ravel() - w2) <= bw)
         assert all(torch.isfinite(t).all() for t in (E, W))
+
+
+def test_calls_at_once_on_two_streams():
+    """The calls that take workspaces, on two streams with nothing between them, against the same calls one after the other."""
+    import torch
+    from paper_2003_11666_amd import embed_backward, log_probs
+    gen = torch.Generator().manual_seed(1)
+    work = []
+    for k in range(2):
+        x = torch.randn(3, 90001, generator=gen).cuda()
+        ids = torch.randint(0, 900, (9000 + k,), generator=gen).cuda()
+        work.append((x, ids, torch.randn(len(ids), 40, generator=gen).cuda()))
+
+    def calls(x, ids, g):
+        out = []
+        for _ in range(5):
+            out += [*log_probs(x, torch.zeros(3, dtype=torch.int64, device="cuda"), top=33), embed_backward(g, ids, torch.empty(900, 40, device="cuda"))]
+        return out
+
+    alone = [calls(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = []
+    for s, w in zip(streams, work):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            both.append(calls(*w))
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
