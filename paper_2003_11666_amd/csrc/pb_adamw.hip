@@ -296,7 +296,7 @@ k_adamw_moments(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v, co
 void launch_adamw(const AdamWArgs& a, int64_t groups, int chunk, int w_type, int g_type, int hat_type, int bits, hipStream_t s) {
   with_type(w_type, [&](auto w) { with_type(g_type, [&](auto g) { with_type(hat_type, [&](auto h) {
     using W = decltype(w); using G = decltype(g); using H = decltype(h);
-    auto f = bits == 32 ? k_adamw<W, G, H, 32, 4096> : chunk == 8192 ? k_adamw<W, G, H, 8, 8192> : k_adamw<W, G, H, 8, 4096>;
+    auto f = bits == 32 ? k_adamw<W, G, H, 32, 2048> : chunk == 8192 ? k_adamw<W, G, H, 8, 8192> : k_adamw<W, G, H, 8, 4096>;
     hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(AT), 0, s, a);
   }); }); });
 }

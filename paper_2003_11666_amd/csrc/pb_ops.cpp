@@ -83,7 +83,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
   int64_t blocks = 0, work = 0;
   for (int32_t i = 0; i < n_tensors; ++i) {
     const pb_adamw_tensor& t = ts[i];
-    if (t.n < 0 || t.n > MOST_GROUPS * 4096 || (blocks += in_blocks(t.n)) > MOST / PB_ADAMW_BLOCK) return fail(PB_E_INVALID, "tensor %d: bad size", (int)i);
+    if (t.n < 0 || t.n > MOST_GROUPS * 2048 || (blocks += in_blocks(t.n)) > MOST / PB_ADAMW_BLOCK) return fail(PB_E_INVALID, "tensor %d: bad size", (int)i);
     if (t.n == 0) continue;
     ++work;
     if (!t.w || !t.g) return fail(PB_E_INVALID, "tensor %d: no weights or no gradient", (int)i);
@@ -141,7 +141,7 @@ int pb_adamw_step(const pb_adamw_tensor* ts, int32_t n_tensors, const pb_adamw_d
 }
 
 int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp, int64_t n, float* m_out, float* v_out, void* stream) {
-  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST_GROUPS * 4096) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
+  if (n < 0 || n % PB_ADAMW_BLOCK || n > MOST_GROUPS * 2048) return fail(PB_E_INVALID, "n must be a multiple of %d", (int)PB_ADAMW_BLOCK);
   if (n == 0) return PB_OK;
   if (!m || !v || !m_exp || !v_exp || !m_out || !v_out) return fail(PB_E_INVALID, "NULL argument");
   if (((uintptr_t)m | (uintptr_t)v | (uintptr_t)m_out | (uintptr_t)v_out) % 16) return fail(PB_E_INVALID, "arrays must be 16-byte aligned");

@@ -18,10 +18,11 @@ constexpr int64_t MOST_GROUPS = (1 << 24) - 1;   // of 256 threads: a launch cou
 
 // ------------------------------------------------------------------------------------------------ AdamW (pb_adamw.hip)
 constexpr int ADAMW_TENSORS = 64;    // tensors per launch: a lane each in the search for a workgroup's tensor, 3 KB of arguments
-// Elements per workgroup.  8-bit moments: a workgroup that goes on to more vectors has their requests under way while it
-// computes (243 million bf16 weights 540 -> 487 us), but 8192 elements are too many where the chip holds all workgroups in two
-// or three rounds (17 million fp32 weights 57 -> 61 us).
-constexpr int adamw_chunk(int bits, int64_t elements) { return bits == 8 && elements >= (int64_t)1 << 26 ? 8192 : 4096; }
+// Elements per workgroup.  32-bit moments: two vectors to a thread (243 million weights 1201 us; 1218 with four, 1247 with
+// eight).  8-bit moments: a workgroup that goes on to more vectors has their requests under way while it computes (243 million
+// bf16 weights 540 -> 487 us), but 8192 elements are too many where the chip holds all workgroups in two or three rounds (17
+// million fp32 weights 57 -> 61 us).
+constexpr int adamw_chunk(int bits, int64_t elements) { return bits == 32 ? 2048 : elements >= (int64_t)1 << 26 ? 8192 : 4096; }
 
 struct AdamWArgs {
   void* w[ADAMW_TENSORS];
