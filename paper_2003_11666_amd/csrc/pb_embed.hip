@@ -351,36 +351,65 @@ __device__ __forceinline__ void sum_chunk(const EmbedGradArgs& a, const Sorted& 
   }
 }
 
-// Zeros into those of the rows r0, r0 + 1, ... of the table whose lane says so.
-template <class O> __device__ __forceinline__ void clear(const EmbedGradArgs& a, int64_t r0, bool empty) {
-  const float zero[EV] = {};
-  Columns<O> zeros;
-  zeros.put(zero);
-  for (uint64_t more = __ballot(empty); more; more &= more - 1) {
-    O* out = (O*)a.d_table + (r0 + __builtin_ctzll(more)) * a.dim;
-    for (int64_t j0 = 0; j0 < a.dim; j0 += SLICE) {
-      const Lane l = columns(j0, a.dim);
-      zeros.store(out + l.j, l);
+__device__ __forceinline__ uint64_t any_lane(uint64_t x) {   // the bits that a lane has
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x |= (uint64_t)__shfl_xor((unsigned long long)x, o, 64);
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// Zeros into those of the rows r0, r0 + 1, ... of the table whose bit is set (the same for all lanes), rows beside each other as one
+// stretch of memory: narrow ones would take a store of a few lanes each.
+template <class O> __device__ __forceinline__ void clear(const EmbedGradArgs& a, int64_t r0, uint64_t empty) {
+  constexpr int V = Sixteen<O>::V;
+  const int lane = threadIdx.x & 63;
+  Sixteen<O> zeros;
+  zeros.q = (typename Sixteen<O>::words){0, 0, 0, 0};
+  while (empty) {
+    const int first = __builtin_ctzll(empty);
+    const uint64_t rest = ~(empty >> first);
+    const int rows = rest ? __builtin_ctzll(rest) : 64;
+    empty &= rows == 64 ? 0 : ~(((1ull << rows) - 1) << first);
+    O* out = (O*)a.d_table + (r0 + first) * a.dim;
+    const int64_t n = rows * a.dim;
+    if (n < V) {
+      if (lane < n) out[lane] = from_float<O>(0.f);
+    } else {
+      for (int64_t j = lane * V; j < n; j += 64 * V) zeros.store(out + (j < n - V ? j : n - V));
     }
   }
 }
 
-// Rows of the table that no token names, `rows` to a wavefront: a lane looks up one of them among the sorted ids.  64 beside many
-// sums (131072 tokens: 102 us, 110 with 16, whose searches take their places), 16 where there is little else to do (259
-// tokens: 58 MB of zeros in 15 us, 19 with 64, 17 with 9).
-int rows_to_clear(int64_t pieces) { return pieces < 4096 ? 16 : 64; }
+// The first of the sorted tokens whose id is `id` or larger, by a wavefront: 64 places tried at a time.
+__device__ __forceinline__ int64_t first_from(const Sorted& s, int64_t id) {
+  const int lane = threadIdx.x & 63;
+  int64_t lo = 0, hi = s.n;
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const int below = (int)__popcll(__ballot(at < hi && (int64_t)s.key[at < hi ? at : lo] < id));   // (the first `below` of them)
+    if (step == 1) return lo + below;
+    if (below == 0) return lo;
+    const int64_t end = lo + below * step;
+    lo = end - step + 1;
+    hi = end < hi ? end : hi;
+  }
+  return lo;
+}
+
+// Rows of the table that no token names, `rows` to a wavefront.
 template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArgs& a, const Sorted& s, int64_t r0, int rows) {
   const int lane = threadIdx.x & 63;
-  const int64_t r = lane < rows ? r0 + lane : a.vocab;
-  int64_t lo = 0, hi = s.n;   // the first sorted token of an id >= r
-  while (__any(lo < hi)) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (lo < hi) {
-      if ((int64_t)s.key[mid] < r) lo = mid + 1;
-      else hi = mid;
-    }
+  uint64_t named = 0;
+  for (int64_t at = first_from(s, r0); at < s.n;) {
+    const int64_t ahead = (int64_t)s.key[at + lane < s.n ? at + lane : s.n - 1] - r0;
+    const int row = ahead < rows ? (int)ahead : rows;
+    named |= any_lane(row < rows ? 1ull << row : 0);
+    const int last = __builtin_amdgcn_readlane(row, 63);
+    if (last == rows || at + 64 >= s.n) break;
+    at = first_from(s, r0 + last + 1);   // (behind an id that many tokens share)
   }
-  clear<O>(a, r0, r < a.vocab && !(lo < s.n && (int64_t)s.key[lo] == r));
+  const int64_t left = a.vocab - r0;
+  const int mine = left < rows ? (int)left : rows;
+  clear<O>(a, r0, ~named & (mine == 64 ? ~0ull : (1ull << mine) - 1));
 }
 
 template <class T, class O, bool ADD>
@@ -461,18 +490,15 @@ __global__ void __launch_bounds__(EB) k_handful(const EmbedGradArgs a, int slice
   for (int64_t p = (int64_t)blockIdx.x * EW + (threadIdx.x >> 6); p < pieces + clears; p += (int64_t)gridDim.x * EW) {
     if (p >= pieces) {
       const int64_t r0 = (p - pieces) * rows;
-      uint64_t named = 0;   // rows that one of the lane's ids names, then of all lanes' ids
+      uint64_t named = 0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const int64_t row = (int64_t)key[r] - r0;
         if (row >= 0 && row < rows) named |= 1ull << row;
       }
-      uint64_t all = 0;
-      for (uint64_t more = __ballot(named != 0); more; more &= more - 1) {
-        const int from = __builtin_ctzll(more);
-        all |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(named >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)named, from);
-      }
-      clear<O>(a, r0, lane < rows && r0 + lane < a.vocab && !(all >> lane & 1));
+      const int64_t left = a.vocab - r0;
+      const int mine = left < rows ? (int)left : rows;
+      clear<O>(a, r0, ~any_lane(named) & (mine == 64 ? ~0ull : (1ull << mine) - 1));
       continue;
     }
     const int i = (int)(p / slices);
@@ -519,6 +545,13 @@ dim3 groups_for(int64_t wavefronts) {
 
 int64_t in_slices(int64_t dim) { return (dim + SLICE - 1) / SLICE; }
 
+// Rows of `bytes` that a wavefront clears: 64 KB of them (60000 rows of 4 KB 42 us, 46 with 32 KB; nothing between them where the
+// rows are short), 64 beside many sums, whose places the searches would take (131072 tokens 136 us, 149 with 16).
+int rows_to_clear(int64_t pieces, int64_t bytes) {
+  const int64_t rows = 65536 / bytes;
+  return pieces >= 4096 || rows > 64 ? 64 : rows < 1 ? 1 : (int)rows;
+}
+
 // Tokens per chunk: 8 at least, and so many that about 4096 wavefronts share the sums, in 512 to 2048 chunks: an id that most
 // tokens share leaves a part in each of them.
 int chunk_of(int64_t n, int64_t dim) {
@@ -559,8 +592,7 @@ int64_t embed_grad_workspace(int64_t n, int64_t, int64_t dim) { return n > HANDF
 void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int id_bits, hipStream_t s) {
   const int64_t slices = in_slices(a.dim);
   if (a.n <= HANDFUL) {
-    // (zeros: no search here, so that as many wavefronts as 8192 may share them: 82 MB in 17 us, 20 with 16 rows to each)
-    const int64_t pieces = a.n * slices, share = (a.vocab + 8191) / 8192, rows = share < 16 ? share : 16, clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
+    const int64_t pieces = a.n * slices, rows = rows_to_clear(pieces, a.dim * (table_dtype == PB_BF16 ? 2 : 4)), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
     with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) { with_id(id_bits, [&](auto id) { with_flag(a.add != 0, [&](auto add) {
       hipLaunchKernelGGL((k_handful<decltype(t), decltype(o), decltype(id), decltype(add)::value>), groups_for(pieces + clears), dim3(EB), 0, s, a, (int)slices, pieces, clears, (int)rows);
     }); }); }); });
@@ -592,7 +624,7 @@ void launch_embed_grad(const EmbedGradArgs& a, int dtype, int table_dtype, int i
     }
   });
   const int chunk = chunk_of(a.n, a.dim);
-  const int64_t chunks = (a.n + chunk - 1) / chunk, rows = rows_to_clear(chunks * slices), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
+  const int64_t chunks = (a.n + chunk - 1) / chunk, rows = rows_to_clear(chunks * slices, a.dim * (table_dtype == PB_BF16 ? 2 : 4)), clears = a.add ? 0 : (a.vocab + rows - 1) / rows;
   const Sorted sorted = {at(l.key[from]), at(l.place[from]), a.n, chunk, (float*)at(l.part)};
   with_type(dtype, [&](auto t) { with_type(table_dtype, [&](auto o) { with_flag(a.add != 0, [&](auto add) {
     constexpr bool ADD = decltype(add)::value;

@@ -172,3 +172,32 @@ def test_tables_beyond_32_bit_offsets():
     # one rounding to bf16 of the result, and one 32-bit one in each of two sums
     bound = 2.0 ** -8 * ref.abs() + 4 * 2.0 ** -24 * (before.abs() + 2 * g.double().abs().max())
     assert torch.all((w[ids[:3]].double() - ref).abs() <= bound)
+
+
+@pytest.mark.parametrize("n", [100, 300, 9000])
+def test_largest_vocabulary(n):
+    """2^31 rows, one column: the first and the last row, ids on both sides of the table, and zeros everywhere else."""
+    import torch
+    from paper_2003_11666_amd import embed_backward
+    vocab = 1 << 31
+    ids = torch.randint(0, vocab, (n,), generator=torch.Generator().manual_seed(n)).cuda()
+    ids[:6] = torch.tensor([0, vocab - 1, vocab, -1, 0, vocab - 1], device="cuda")
+    g = torch.randint(1, 8, (n, 1), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()      # (small whole numbers: sums are exact)
+    d = torch.full((vocab, 1), 3.0, dtype=torch.bfloat16, device="cuda")
+    embed_backward(g, ids, d)
+    there = (ids >= 0) & (ids < vocab)
+    rows, place = ids[there].unique(return_inverse=True)
+    ref = torch.zeros(len(rows), device="cuda").index_add_(0, place, g[there][:, 0].float())
+    assert torch.equal(d[rows, 0].float(), ref)
+    d[rows] = 0
+    assert sum(int(torch.count_nonzero(d[at:at + (1 << 28)])) for at in range(0, vocab, 1 << 28)) == 0
+
+
+def test_rows_between_ids_that_many_tokens_share():
+    """Ids so frequent that the sorted tokens of one are passed over between two rows of zeros."""
+    import torch
+    vocab = 130
+    ids = torch.tensor([5] * 300 + [6] * 3 + [70] * 500 + [129] * 70 + [7, 64, 63, 0]).cuda()
+    ids = ids[torch.randperm(len(ids), generator=torch.Generator().manual_seed(0)).cuda()]
+    for dim in (1, 3, 8, 17, 520):
+        check_grad(table(len(ids), dim, "float32"), ids, torch.full((vocab, dim), 2.0, device="cuda"), add=False)
