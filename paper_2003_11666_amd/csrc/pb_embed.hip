@@ -411,17 +411,29 @@ __device__ __forceinline__ int64_t first_from(const Sorted& s, int64_t id) {
   return lo;
 }
 
-// Rows of the table that no token names, `rows` to a wavefront.
+// Rows of the table that no token names, `rows` to a wavefront.  Their tokens are 64 of the sorted ones at most where ids are rare;
+// where they are not, each lane looks a row of its own up.
 template <class O> __device__ __forceinline__ void clear_rows(const EmbedGradArgs& a, const Sorted& s, int64_t r0, int rows) {
   const int lane = threadIdx.x & 63;
+  int64_t lo = first_from(s, r0), hi = s.n;
   uint64_t named = 0;
-  for (int64_t at = first_from(s, r0); at < s.n;) {
-    const int64_t ahead = (int64_t)s.key[at + lane < s.n ? at + lane : s.n - 1] - r0;
+  if (lo < hi) {
+    const int64_t ahead = (int64_t)s.key[lo + lane < hi ? lo + lane : hi - 1] - r0;
     const int row = ahead < rows ? (int)ahead : rows;
-    named |= any_lane(row < rows ? 1ull << row : 0);
-    const int last = __builtin_amdgcn_readlane(row, 63);
-    if (last == rows || at + 64 >= s.n) break;
-    at = first_from(s, r0 + last + 1);   // (behind an id that many tokens share)
+    if (__builtin_amdgcn_readlane(row, 63) == rows || lo + 64 >= hi) {
+      named = any_lane(row < rows ? 1ull << row : 0);
+    } else {
+      const int64_t r = r0 + lane;
+      while (__any(lo < hi)) {
+        const int64_t mid = (lo + hi) >> 1;
+        const bool below = (int64_t)s.key[mid < s.n ? mid : s.n - 1] < r;
+        if (lo < hi) {
+          if (below) lo = mid + 1;
+          else hi = mid;
+        }
+      }
+      named = __ballot(lane < rows && lo < s.n && (int64_t)s.key[lo < s.n ? lo : s.n - 1] == r);
+    }
   }
   const int64_t left = a.vocab - r0;
   const int mine = left < rows ? (int)left : rows;
