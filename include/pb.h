@@ -380,15 +380,15 @@ int pb_log_probs_backward(const void* logits, int32_t dtype, int64_t rows, int64
                           const float* g_logp, const float* g_entropy, void* dlogits, int64_t d_stride, void* stream);
 
 /* Embeddings.  out[i] = scale * table[ids[i]], rounded once to out_dtype: n rows of dim elements, one after the
- * other, from a table of vocab rows.  An id outside [0, vocab) (padding) gives a row of zeros. */
+ * other, from a table of vocab rows, dim < 2^31.  An id outside [0, vocab) (padding) gives a row of zeros. */
 int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const void* ids, int32_t id_bits, int64_t n,
              float scale, void* out, int32_t out_dtype, void* stream);
 
 /* Gradient of the table: for each row, scale * the sum of the rows of d_out (n rows of dim, type `dtype`) whose
  * id is that row's, added up in 32 bits in the order of their places.  add = 0: d_table (vocab rows of dim, type
  * table_dtype) is written, with zeros in rows that no id names; add = 1: the sums are added to it, and rows that no
- * id names are left alone.  d_out and d_table must not overlap.  n <= 2^30, vocab <= 2^31.  `workspace`: pb_embed_backward_workspace bytes, 16-byte
- * aligned, free for other use when the call's work is done. */
+ * id names are left alone.  d_out and d_table must not overlap.  n <= 2^30, vocab <= 2^31, dim < 2^31.  `workspace`: pb_embed_backward_workspace bytes
+ * (NULL where that is 0), 16-byte aligned, free for other use when the call's work is done. */
 int64_t pb_embed_backward_workspace(int64_t n, int64_t vocab, int64_t dim);
 int pb_embed_backward(const void* d_out, int32_t dtype, const void* ids, int32_t id_bits, int64_t n, int64_t vocab,
                       int64_t dim, float scale, void* d_table, int32_t table_dtype, int32_t add, void* workspace,

@@ -200,7 +200,7 @@ int pb_log_probs_backward(const void* logits, int32_t dtype, int64_t rows, int64
 int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const void* ids, int32_t id_bits, int64_t n, float scale, void* out,
              int32_t out_dtype, void* stream) {
   if (!is_type(dtype) || !is_type(out_dtype)) return fail(PB_E_INVALID, "types must be PB_F32 or PB_BF16");
-  if (vocab <= 0 || !is_matrix(vocab, dim, dim) || !is_matrix(n, dim, dim)) return fail(PB_E_INVALID, "bad sizes: a table of %lld rows of %lld, %lld ids", (long long)vocab, (long long)dim, (long long)n);
+  if (vocab <= 0 || dim > 0x7fffffff || !is_matrix(vocab, dim, dim) || !is_matrix(n, dim, dim)) return fail(PB_E_INVALID, "bad sizes: a table of %lld rows of %lld, %lld ids", (long long)vocab, (long long)dim, (long long)n);
   if (const int rc = bad_ids("ids", ids, id_bits)) return rc;
   if (n == 0) return PB_OK;
   if (!table || !ids || !out) return fail(PB_E_INVALID, "NULL argument");
@@ -210,7 +210,7 @@ int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const
 }
 
 int64_t pb_embed_backward_workspace(int64_t n, int64_t vocab, int64_t dim) {
-  if (vocab <= 0 || vocab > (int64_t)1 << 31 || n > (int64_t)1 << 30 || !is_matrix(vocab, dim, dim) || !is_matrix(n, dim, dim)) return fail(PB_E_INVALID, "bad sizes");
+  if (vocab <= 0 || vocab > (int64_t)1 << 31 || n > (int64_t)1 << 30 || dim > 0x7fffffff || !is_matrix(vocab, dim, dim) || !is_matrix(n, dim, dim)) return fail(PB_E_INVALID, "bad sizes");
   return embed_grad_workspace(n, vocab, dim);
 }
 

@@ -128,7 +128,7 @@ def test_log_probs_backward_refuses(kw, text):
 
 @pytest.mark.parametrize("kw,text", [
     (dict(dtype=2), "types"), (dict(out_dtype=2), "types"), (dict(vocab=0), "bad sizes"), (dict(dim=0), "bad sizes"), (dict(n=-1), "bad sizes"),
-    (dict(n=1 << 40, dim=1 << 20), "bad sizes"), (dict(id_bits=0), "32 or 64"), (dict(ids=A + 4), "boundaries"), (dict(table=None), "NULL"),
+    (dict(n=1 << 40, dim=1 << 20), "bad sizes"), (dict(dim=1 << 31), "bad sizes"), (dict(id_bits=0), "32 or 64"), (dict(ids=A + 4), "boundaries"), (dict(table=None), "NULL"),
     (dict(ids=None), "NULL"), (dict(out=None), "NULL"), (dict(out=A + 2), "boundaries"),
 ])
 def test_embed_refuses(kw, text):
@@ -138,7 +138,7 @@ def test_embed_refuses(kw, text):
 
 @pytest.mark.parametrize("kw,text", [
     (dict(dtype=2), "types"), (dict(table_dtype=2), "types"), (dict(add=2), "add"), (dict(vocab=0), "bad sizes"), (dict(vocab=(1 << 31) + 1), "bad sizes"),
-    (dict(n=(1 << 30) + 1), "bad sizes"), (dict(dim=0), "bad sizes"), (dict(id_bits=1), "32 or 64"), (dict(ids=A + 4), "boundaries"), (dict(d_out=None), "NULL"),
+    (dict(n=(1 << 30) + 1), "bad sizes"), (dict(dim=0), "bad sizes"), (dict(dim=1 << 31), "bad sizes"), (dict(id_bits=1), "32 or 64"), (dict(ids=A + 4), "boundaries"), (dict(d_out=None), "NULL"),
     (dict(ids=None), "NULL"), (dict(d_table=None), "NULL"), (dict(d_table=A + 2), "boundaries"), (dict(ws=None), "workspace"), (dict(ws_bytes=1), "workspace"),
     (dict(ws=A + 8), "workspace"),
 ])
