@@ -277,3 +277,14 @@ def test_refusals_of_tensors_on_the_gpu():
         a = {**dict(params=[w], grads=[w], m=m, v=m.clone(), step=1, lr=0.1), **kw}
         with pytest.raises(PBError):
             adamw_step(a.pop("params"), a.pop("grads"), a.pop("m"), a.pop("v"), **a)
+
+
+@pytest.mark.parametrize("bits", ["32", "8"])
+def test_update_bench_measures_it(bits, monkeypatch, capsys):
+    import json
+    import sys
+    from paper_2003_11666_amd import update_bench
+    monkeypatch.setattr(sys, "argv", ["update_bench", "--elements", str(1 << 16), "--reps", "2", "--adamw", bits])
+    update_bench.main()
+    out = json.loads(capsys.readouterr().out)
+    assert out["adamw_moment_bits"] == int(bits) and out["adamw_us"] > 0 and out["update_us"] > 0
