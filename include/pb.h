@@ -360,6 +360,7 @@ int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, c
  * its logp is 0.  A row whose logits are all -inf has no distribution: M = -inf, ln s = 0, entropy 0, the log
  * probability of each token -inf.  A NaN, or +inf, makes the row's results NaN; a NaN counts as the largest logit in
  * the order of the alternatives.  entropy may be NULL; targets and logp both NULL: no token is given.
+ * The last bits of a row's sums may depend on how many rows the call has (few long ones are shared out differently).
  * 0 < scale (one over a temperature), 0 <= top <= min(vocab, PB_TOP_MAX), vocab < 2^31, row_stride >= vocab.
  * `workspace`: pb_log_probs_workspace bytes (NULL where that is 0), 16-byte aligned, free for other use when the
  * call's work is done. */

@@ -1,6 +1,7 @@
 """Operators over plain device tensors: AdamW over many tensors at once, log probabilities of given tokens and their
 gradient, embedding lookup and its gradient (the functions of include/pb.h beside pb_update_standalone, which defines them).
-Argument marshalling and checks only; PyTorch provides the memory and the stream.  Nothing here is recorded by autograd."""
+Argument marshalling and checks only; PyTorch provides the memory and the stream.  Nothing here is recorded by autograd, and
+what a call writes in place (weights, moments, a table's gradient) is written through its address: autograd does not notice."""
 from __future__ import annotations
 
 import ctypes as C

@@ -29,10 +29,11 @@ def _mix(z):
     return z ^ (z >> np.uint64(31))
 
 
-def dither(n, seed, step):
+def dither(n, seed, step, start=0):
+    """Of the elements from place `start` on."""
     with np.errstate(over="ignore"):
         key = _mix(np.array([seed], np.uint64) ^ _mix(np.array([step], np.uint64)))
-        i = np.arange(n, dtype=np.uint64)
+        i = np.arange(n, dtype=np.uint64) + np.uint64(start)
         z = _mix((i >> np.uint64(1)) * np.uint64(0x9E3779B97F4A7C15) + key) >> (np.uint64(32) * (i & np.uint64(1)))
     return ((z & np.uint64(0xFFFF)).astype(np.int64) << 4 | 8), ((z >> np.uint64(16) & np.uint64(0xFFFF)).astype(np.int64) << 4 | 8)
 

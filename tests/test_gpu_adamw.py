@@ -288,3 +288,22 @@ def test_update_bench_measures_it(bits, monkeypatch, capsys):
     update_bench.main()
     out = json.loads(capsys.readouterr().out)
     assert out["adamw_moment_bits"] == int(bits) and out["adamw_us"] > 0 and out["update_us"] > 0
+
+
+def test_predicted_weights_of_some_tensors_only():
+    """The C entry takes w_hat tensor by tensor."""
+    import ctypes as C
+    import torch
+    from paper_2003_11666_amd import operators as P
+    lib = P._library()
+    w, g = [torch.randn(300, device="cuda") for _ in range(3)], [torch.randn(300, device="cuda") for _ in range(3)]
+    hat = torch.full((300,), 5.0, device="cuda")
+    m, v = torch.zeros(3 * 384, device="cuda"), torch.zeros(3 * 384, device="cuda")
+    rec = np.zeros(3, dtype=P._TENSOR)
+    rec["w"], rec["g"], rec["n"] = [t.data_ptr() for t in w], [t.data_ptr() for t in g], 300
+    rec["w_hat"][1] = hat.data_ptr()
+    d = P._AdamWDesc(moment_bits=32, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
+    torch.cuda.synchronize()
+    assert lib.pb_adamw_step(rec.ctypes.data, 3, C.byref(d), m.data_ptr(), v.data_ptr(), None, None, None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(hat, w[1])
