@@ -158,12 +158,12 @@ def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, w
             setattr(d, name, _type(ts[0], "adamw_step: tensors"))
     at = list(map(T.data_ptr, every))
     rec = np.zeros(n, dtype=_TENSOR)
-    if np.ndim(weight_decay) and np.shape(weight_decay) != (n,):
+    if not isinstance(weight_decay, (int, float)) and len(weight_decay) != n:
         raise PBError("adamw_step: weight_decay must be a number, or one for each parameter")
     rec["w"], rec["g"], rec["n"], rec["weight_decay"] = at[:n], at[n:2 * n], sizes[:n], weight_decay
     if hats:
         rec["w_hat"] = at[2 * n:]
-    total = int((-(-rec["n"] // ADAMW_BLOCK) * ADAMW_BLOCK).sum())
+    total = int(((rec["n"] + ADAMW_BLOCK - 1) // ADAMW_BLOCK).sum()) * ADAMW_BLOCK
     eight = m.dtype == torch.uint8
     if v.dtype != m.dtype or m.dtype not in (torch.uint8, torch.float32) or m.numel() != total or v.numel() != total:
         raise PBError(f"adamw_step: m and v must be flat float32 or uint8 of {total} elements")
