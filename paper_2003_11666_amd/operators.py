@@ -158,7 +158,7 @@ def adamw_step(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps=1e-8, w
             setattr(d, name, _type(ts[0], "adamw_step: tensors"))
     at = list(map(T.data_ptr, every))
     rec = np.zeros(n, dtype=_TENSOR)
-    if not isinstance(weight_decay, (int, float)) and len(weight_decay) != n:
+    if len(weight_decay) != n if isinstance(weight_decay, (list, tuple)) else np.shape(weight_decay) not in ((), (n,)):
         raise PBError("adamw_step: weight_decay must be a number, or one for each parameter")
     rec["w"], rec["g"], rec["n"], rec["weight_decay"] = at[:n], at[n:2 * n], sizes[:n], weight_decay
     if hats:

@@ -268,6 +268,17 @@ def test_step_number_of_the_host_and_of_the_gpu_agree(bits):
         assert torch.allclose(a["w"][0], b["w"][0], rtol=4 * 2.0 ** -24, atol=4 * 2.0 ** -24)
 
 
+def test_forms_of_weight_decay():
+    from paper_2003_11666_amd import adamw_step
+    ref = None
+    for wd in (0.25, np.float32(0.25), [0.25, 0.25], (0.25, 0.25), np.array([0.25, 0.25])):
+        s = make((300, 77))
+        adamw_step(s["w"], s["g"], s["m"], s["v"], step=1, lr=0.5, weight_decay=wd)
+        got = flat(s["w"], s["sizes"])
+        assert ref is None or np.array_equal(got, ref)
+        ref = got
+
+
 def test_refusals_of_tensors_on_the_gpu():
     import torch
     from paper_2003_11666_amd import PBError, adamw_step
