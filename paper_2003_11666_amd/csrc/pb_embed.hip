@@ -218,20 +218,25 @@ __global__ void __launch_bounds__(RB) k_rank(const ID* ids, int n, int64_t vocab
 }
 
 // One pass over more tokens, in tiles: how often each digit occurs in each tile ...
-template <class ID, bool FIRST>
-__device__ __forceinline__ uint32_t key_at(const void* in, int64_t i, int64_t vocab) { return FIRST ? id_key(((const ID*)in)[i], vocab) : ((const uint32_t*)in)[i]; }
+// (In all of these what a thread needs from memory is requested first, and none of it behind a branch.)
+template <class ID, bool FIRST> struct Key {
+  typename std::conditional<FIRST, ID, uint32_t>::type x;
+  __device__ __forceinline__ void load(const void* in, int64_t i, int64_t n) { x = ((const decltype(x)*)in)[i < n ? i : n - 1]; }
+  __device__ __forceinline__ uint32_t get(int64_t vocab) const { return FIRST ? id_key(x, vocab) : (uint32_t)x; }
+};
 
 template <class ID, bool FIRST>
 __global__ void __launch_bounds__(EB) k_digits(const void* in, int64_t n, int64_t vocab, int shift, int width, int64_t tiles, uint32_t* counts) {
   __shared__ uint32_t count[BINS];
+  const int64_t i0 = (int64_t)blockIdx.x * TILE + threadIdx.x;
+  Key<ID, FIRST> k[TILE / EB];
+#pragma unroll
+  for (int g = 0; g < TILE / EB; ++g) k[g].load(in, i0 + g * EB, n);
   for (int i = threadIdx.x; i < BINS; i += EB) count[i] = 0;
   __syncthreads();
-  const int64_t i0 = (int64_t)blockIdx.x * TILE;
 #pragma unroll
-  for (int g = 0; g < TILE / EB; ++g) {
-    const int64_t i = i0 + g * EB + threadIdx.x;
-    if (i < n) atomicAdd(&count[key_at<ID, FIRST>(in, i, vocab) >> shift & ((1u << width) - 1)], 1u);
-  }
+  for (int g = 0; g < TILE / EB; ++g)
+    if (i0 + g * EB < n) atomicAdd(&count[k[g].get(vocab) >> shift & ((1u << width) - 1)], 1u);
   __syncthreads();
   for (int i = threadIdx.x; i < 1 << width; i += EB) counts[i * tiles + blockIdx.x] = count[i];
 }
@@ -261,32 +266,44 @@ k_scatter(const void* in, const uint32_t* place_in, int64_t n, int64_t vocab, in
   __shared__ uint32_t count[EW][BINS], part[EW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
   constexpr int G = TILE / EB;
-  for (int i = tid; i < EW * BINS; i += EB) (&count[0][0])[i] = 0;
   const int64_t i0 = (int64_t)blockIdx.x * TILE + wave * (TILE / EW) + lane;
   const uint32_t mask = (1u << width) - 1;
-  uint32_t k[G], p[G], r[G], digit[G];
+  Key<ID, FIRST> x[G];
+  uint32_t k[G], p[G], r[G], digit[G], t[2], ahead[2];
   bool mine[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    const int64_t i = i0 + g * 64;
-    mine[g] = i < n;
-    k[g] = mine[g] ? key_at<ID, FIRST>(in, i, vocab) : 0;
-    p[g] = FIRST || !mine[g] ? (uint32_t)i : place_in[i];
+    x[g].load(in, i0 + g * 64, n);
+    p[g] = FIRST ? 0 : place_in[i0 + g * 64 < n ? i0 + g * 64 : n - 1];
+  }
+  // two digits to a thread: how many tokens have them, and how many in the tiles before
+  static_assert(BINS == 2 * EB, "two digits to a thread");
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int d = 2 * tid + h <= (int)mask ? 2 * tid + h : 0;
+    t[h] = total[d];
+    ahead[h] = counts[d * tiles + blockIdx.x];
+  }
+  for (int i = tid; i < EW * BINS; i += EB) (&count[0][0])[i] = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    mine[g] = i0 + g * 64 < n;
+    k[g] = x[g].get(vocab);
+    if (FIRST) p[g] = (uint32_t)(i0 + g * 64);
     digit[g] = k[g] >> shift & mask;
   }
   __syncthreads();
   places_in_wave<G>(digit, mine, count[wave], r);
   __syncthreads();
-  // the first place of each digit's tokens of each wavefront: two digits to a thread
-  static_assert(BINS == 2 * EB, "two digits to a thread");
-  uint32_t t[2];
+  // the first place of each digit's tokens of each wavefront
 #pragma unroll
-  for (int h = 0; h < 2; ++h) t[h] = 2 * tid + h <= (int)mask ? total[2 * tid + h] : 0;
+  for (int h = 0; h < 2; ++h)
+    if (2 * tid + h > (int)mask) t[h] = ahead[h] = 0;
   uint32_t at = sum_before<EW>(t[0] + t[1], part);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int d = 2 * tid + h;
-    uint32_t a = at + (d <= (int)mask ? counts[d * tiles + blockIdx.x] : 0);
+    uint32_t a = at + ahead[h];
     at += t[h];
 #pragma unroll
     for (int w = 0; w < EW; ++w) {
@@ -460,13 +477,15 @@ __global__ void __launch_bounds__(JB) k_join(const EmbedGradArgs a, const Sorted
   const int64_t c = blockIdx.x, lo = c * s.chunk, hi = lo + s.chunk;
   if (hi >= s.n) return;
   const uint32_t id = s.key[hi - 1], then = s.key[hi], first = s.key[lo], before = lo > 0 ? s.key[lo - 1] : 0xFFFFFFFFu;
+  uint32_t start = s.key[hi + (int64_t)lane * s.chunk < s.n ? hi + (int64_t)lane * s.chunk : s.n - 1];   // of each of the next 64 chunks
   if (id >= (uint64_t)a.vocab || then != id || (first == id && before == id)) return;
   int64_t behind = 0;   // chunks behind this one that go on with the id
   for (;;) {
-    const int64_t at = (c + 1 + behind + lane) * s.chunk;
-    const uint64_t on = __ballot(at < s.n && s.key[at < s.n ? at : 0] == id);
+    const uint64_t on = __ballot(hi + (behind + lane) * s.chunk < s.n && start == id);
     behind += on == ~0ull ? 64 : __builtin_ctzll(~on);
     if (on != ~0ull) break;
+    const int64_t at = hi + (behind + lane) * s.chunk;
+    start = s.key[at < s.n ? at : s.n - 1];
   }
   for (int64_t j0 = (int64_t)blockIdx.y * SLICE; j0 < a.dim; j0 += (int64_t)gridDim.y * SLICE) {
     const Lane l = columns(j0, a.dim);
