@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a, int64_t pieces,
 // Stable, by digits of the id from the lowest up; an id outside the table becomes `vocab`, behind all others.  Digits are as
 // wide as the fewest passes make them, 9 bits at most: two passes for up to 2^18 ids.
 constexpr int DIGIT = 9, BINS = 1 << DIGIT;
-constexpr int FEW = 8192;           // up to so many tokens are ranked by comparisons
+constexpr int FEW = 8192;           // up to so many tokens are ranked by comparisons (11 us, 25 by radix; 12000: 40 and 32 with all else)
 constexpr int TILE = 1024;          // tokens per workgroup of a pass over more
 template <class ID> __device__ __forceinline__ uint32_t id_key(ID id, int64_t vocab) { return (uint32_t)(id >= 0 && (int64_t)id < vocab ? (int64_t)id : vocab); }
 
@@ -150,8 +150,8 @@ template <int WAVES> __device__ __forceinline__ uint32_t sum_before(uint32_t x, 
 // Few tokens: the place of one is how many come before it, each counted against all others.  A workgroup holds the ids of all
 // tokens in LDS, dealt out to 128 parts of its threads, and takes 32 tokens, four to a lane in each part: two instructions
 // for 64 comparisons and an LDS read for sixteen times as many (with one token to a lane these reads were the bound).  The 67
-// million comparisons of 8192 tokens take the chip 3.4 us; a radix sort in one workgroup took 31 us, one in tiles takes six
-// launches.
+// million comparisons of 8192 tokens take the chip 3.4 us, the launch 11; a radix sort in one workgroup took 31 us, one in
+// tiles takes six launches.
 constexpr int RANKED = 32, PER_LANE = 4, RB = 1024, PARTS = RB * PER_LANE / RANKED;
 __device__ __forceinline__ int spread(int j) { return j + (j >> 5) * 4; }   // (parts start at other banks)
 template <class ID>
