@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(EB) k_embed(const EmbedArgs a, int64_t pieces,
 // Stable, by digits of the id from the lowest up; an id outside the table becomes `vocab`, behind all others.  Digits are as
 // wide as the fewest passes make them, 9 bits at most: two passes for up to 2^18 ids.
 constexpr int DIGIT = 9, BINS = 1 << DIGIT;
-constexpr int FEW = 8192;           // up to so many tokens are ranked by comparisons (11 us, 25 by radix; 12000: 40 and 32 with all else)
+constexpr int FEW = 8192;           // up to so many tokens are ranked by comparisons (64 columns added, with all else: 22 us, 33 by radix; 12000: 36, 34)
 constexpr int TILE = 1024;          // tokens per workgroup of a pass over more
 template <class ID> __device__ __forceinline__ uint32_t id_key(ID id, int64_t vocab) { return (uint32_t)(id >= 0 && (int64_t)id < vocab ? (int64_t)id : vocab); }
 
