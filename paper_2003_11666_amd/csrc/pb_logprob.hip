@@ -8,7 +8,6 @@ namespace pb {
 
 constexpr int LB = 256;             // threads per workgroup: 4 wavefronts
 constexpr int WAVES = LB / 64;
-constexpr int64_t SHORT_ROW = 2048; // rows up to here are a wavefront's each
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // ------------------------------------------------------------------------------------------------------- running sums
@@ -245,8 +244,9 @@ template <bool TOP> __device__ __forceinline__ void join_waves(Sums& a, Best& be
 // What a workgroup that takes a part of a row leaves for the one that joins them: its sums, then its alternatives.
 __host__ __device__ __forceinline__ size_t part_bytes(int top) { return 16 + 8 * (size_t)top; }
 
-// Bound by memory: a row is read once.  A row to a wavefront (short ones), to a workgroup, or in `parts` of `part` logits to a
-// workgroup each.
+// Bound by memory: a row is read once (4096 rows of 32768 fp32 84 us, 6.4 TB/s).  A row to a wavefront (short ones), to a workgroup,
+// or in `parts` of `part` logits to a workgroup each.  Alternatives cost a comparison for each logit, and sorting: 512 rows of
+// 200000 bf16 46 us, 68 with 5 of them, 93 with 64.
 template <class T, class ID, bool TOP>
 __global__ void __launch_bounds__(LB) k_logp_short(const LogpArgs a) {
   __shared__ uint64_t lds[WAVES][128];
@@ -316,7 +316,8 @@ __global__ void __launch_bounds__(LB) k_logp_join(const LogpArgs a, int parts) {
 }
 
 // ----------------------------------------------------------------------------------------------------------- gradient
-// Bound by memory: each logit read and its gradient written once.  A wavefront takes U vectors of 16 bytes a lane of one row, whose
+// Bound by memory: each logit read and its gradient written once (8192 rows of 131072 bf16 727 us, 5.9 TB/s; with stores through
+// the caches 755).  A wavefront takes U vectors of 16 bytes a lane of one row, whose
 // numbers are the same for all of its lanes.
 template <class T, class ID, bool ENT>
 __global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t pieces, int per_row) {
@@ -366,12 +367,18 @@ __global__ void __launch_bounds__(LB) k_logp_grad(const LogpGradArgs a, int64_t 
 }
 
 // ------------------------------------------------------------------------------------------------------------ launches
-// A long row among few is dealt out in parts so that the chip has about 1024 workgroups, four to a compute unit, and a thread one
-// vector of its own at least.
+// A row to a wavefront: up to 2048 logits, 4096 among many rows (4096 of 3000 fp32 8.9 us, 10.9 with a workgroup to each; 64 of
+// 3000 bf16 with 5 alternatives 8.1 and 7.0).
+bool short_rows(int64_t rows, int64_t vocab) { return vocab <= 2048 || (vocab <= 4096 && rows >= 1024); }
+
+// A row to a workgroup up to 16384 logits (512 rows of 12000 with 5 alternatives 11.2 us, 15.3 in parts; 64 of 32768 with 20 14.3
+// in parts, 21.8 whole), and where rows are many.  Else it is dealt out in parts, a vector to a thread at least, so that the chip
+// has about 1024 workgroups (300 rows of 200000 with 64 alternatives 71 us; 82 with 512, 77 with 2048).
+constexpr int64_t WHOLE_ROW = 16384, WANTED = 1024;
 struct Split { int parts, part; };
 Split split(int64_t rows, int64_t vocab) {
-  if (vocab <= SHORT_ROW) return {1, (int)vocab};
-  const int64_t want = (1024 + rows - 1) / rows, grain = LB * 8, most = (vocab + grain - 1) / grain;
+  if (vocab <= WHOLE_ROW) return {1, (int)vocab};
+  const int64_t want = (WANTED + rows - 1) / rows, grain = LB * 8, most = (vocab + grain - 1) / grain;
   const int64_t parts = want < most ? want : most, part = ((vocab + parts - 1) / parts + grain - 1) / grain * grain;
   return {(int)((vocab + part - 1) / part), (int)part};
 }
@@ -389,7 +396,7 @@ void launch_logp(const LogpArgs& a, int dtype, int id_bits, hipStream_t s) {
   with_type(dtype, [&](auto t) { with_id(id_bits, [&](auto id) { with_flag(a.top > 0, [&](auto top) {
     using T = decltype(t); using ID = decltype(id);
     constexpr bool TOP = decltype(top)::value;
-    if (a.vocab <= SHORT_ROW) {
+    if (short_rows(a.rows, a.vocab)) {
       hipLaunchKernelGGL((k_logp_short<T, ID, TOP>), groups_for((a.rows + WAVES - 1) / WAVES), dim3(LB), 0, s, a);
       return;
     }

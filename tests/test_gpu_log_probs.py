@@ -74,7 +74,7 @@ def test_vocabularies(vocab, dtype):
         check(logits(rows, vocab, dtype, seed=5), targets(rows, vocab, 32))
 
 
-@pytest.mark.parametrize("rows,vocab", [(1, 200003), (3, 131072), (700, 3000), (5000, 33), (2048, 1001)])
+@pytest.mark.parametrize("rows,vocab", [(1, 200003), (3, 131072), (700, 3000), (5000, 33), (2048, 1001), (1100, 2049), (1100, 4096), (1100, 4097), (3, 16384), (3, 16385)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_rows(rows, vocab, dtype):
     check(logits(rows, vocab, dtype, std=1.5), targets(rows, vocab, 32), top=8)

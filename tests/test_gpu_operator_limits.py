@@ -83,13 +83,14 @@ def test_a_row_in_more_parts_than_a_workgroup_has_lanes():
     check(logits(2, 1200007, "float32", masked=0.5), torch.tensor([5, 1200006], device="cuda"), top=7)
 
 
-def test_more_long_rows_than_a_launch_has_workgroups():
-    """2^20 + 3 rows of 2050 logits, which repeat after 2048 (enough for a workgroup to each as well): so must their results."""
+@pytest.mark.parametrize("vocab", [3001, 4101])
+def test_more_long_rows_than_a_launch_has_workgroups(vocab):
+    """2^20 + 3 rows, which repeat after 2048 (enough for them to be taken in the same way): so must their results."""
     import torch
     from paper_2003_11666_amd import log_probs
     from tests.test_gpu_log_probs import logits
     n, m = (1 << 20) + 3, 2048
-    few = logits(m, 2050, "bfloat16")
+    few = logits(m, vocab, "bfloat16")
     x = few.repeat(n // m + 1, 1)[:n]
     t = torch.arange(n, device="cuda") % m
     a, b = log_probs(x, t, top=2), log_probs(few, t[:m], top=2)
