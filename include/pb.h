@@ -305,7 +305,7 @@ typedef enum { PB_F32 = 0, PB_BF16 = 1 } pb_dtype;
  * (c + 8 (e - 15)) << 20 with the code's top bit as sign; c = 0, or a pattern
  * that is not positive, stands for 0.  v reaches 2^-31 of its block's maximum
  * and is never rounded to 0 (a weight whose v were 0 would take a step of
- * m / eps), m reaches 2^-15.  Rounding is stochastic, up with the probability
+ * m / eps), m reaches 2^-15 and is 0 below.  Rounding is stochastic, up with the probability
  * of the part that is cut off, by 16 bits for each of m and v from a splitmix64
  * stream of (seed, t, the element's place in the flat arrays): rounding to
  * nearest would hold v fast, since one step with beta2 = 0.999 moves it by far
@@ -326,7 +326,7 @@ typedef struct {
 typedef struct {
   int32_t w_type, g_type, w_hat_type;   /* pb_dtype, the same for all tensors of a call */
   int32_t moment_bits;                  /* 32 or 8                                      */
-  double lr, beta1, beta2, eps;         /* lr, eps >= 0; 0 <= beta < 1                  */
+  double lr, beta1, beta2, eps;         /* lr >= 0, eps > 0, 0 <= beta < 1, as 32-bit numbers too */
   double horizon;
   int64_t step;                         /* t >= 1; not looked at where step_dev is given */
   const int64_t* step_dev;              /* t in device memory, read when the step runs (a captured step counts on); or NULL */
@@ -358,8 +358,8 @@ int pb_adamw_moments(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, c
  *                                         index first, and their log probabilities
  * targets and top_ids are of id_bits (32 or 64) bits.  A target outside [0, vocab) marks a row that has none:
  * its logp is 0.  A row whose logits are all -inf has no distribution: M = -inf, ln s = 0, entropy 0, the log
- * probability of each token -inf.  A NaN, or +inf, makes the row's results NaN; a NaN counts as the largest logit in
- * the order of the alternatives.  entropy may be NULL; targets and logp both NULL: no token is given.
+ * probability of each token -inf.  A NaN, or +inf, makes the row's results NaN (but the 0 of a row without a target); a
+ * NaN counts as the largest logit in the order of the alternatives.  entropy may be NULL; targets and logp both NULL: no token is given.
  * The last bits of a row's sums may depend on how many rows the call has (few long ones are shared out differently).
  * 0 < scale (one over a temperature), 0 <= top <= min(vocab, PB_TOP_MAX), vocab < 2^31, row_stride >= vocab.
  * `workspace`: pb_log_probs_workspace bytes (NULL where that is 0), 16-byte aligned, free for other use when the
@@ -374,8 +374,8 @@ int pb_log_probs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab,
  *   dlogits[j] = scale ( g_logp ([j = target] - p_j) - g_entropy p_j (ln p_j + entropy) )
  * in the type of the logits, rounded once; rows d_stride elements apart.  norm, entropy: what pb_log_probs wrote
  * for these logits.  g_logp NULL (then targets are not looked at) or g_entropy NULL (then entropy is not): no such term.
- * A row without a target has no first term; a row whose logits are all -inf has a gradient of 0.  dlogits may be the logits' own array,
- * if d_stride = row_stride, and must not overlap it otherwise. */
+ * A row without a target has no first term; a row whose logits are all -inf has a gradient of 0.  dlogits may be
+ * the logits' own array, if d_stride = row_stride, and must not overlap it otherwise. */
 int pb_log_probs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
                           const void* targets, int32_t id_bits, float scale, const float* norm, const float* entropy,
                           const float* g_logp, const float* g_entropy, void* dlogits, int64_t d_stride, void* stream);
@@ -386,10 +386,11 @@ int pb_embed(const void* table, int32_t dtype, int64_t vocab, int64_t dim, const
              float scale, void* out, int32_t out_dtype, void* stream);
 
 /* Gradient of the table: for each row, scale * the sum of the rows of d_out (n rows of dim, type `dtype`) whose
- * id is that row's, added up in 32 bits in the order of their places.  add = 0: d_table (vocab rows of dim, type
- * table_dtype) is written, with zeros in rows that no id names; add = 1: the sums are added to it, and rows that no
- * id names are left alone.  d_out and d_table must not overlap.  n <= 2^30, vocab <= 2^31, dim < 2^31.  `workspace`: pb_embed_backward_workspace bytes
- * (NULL where that is 0), 16-byte aligned, free for other use when the call's work is done. */
+ * id is that row's, added up in 32 bits in an order that their places fix.  add = 0: d_table (vocab rows of dim,
+ * type table_dtype) is written, with zeros in rows that no id names; add = 1: the sums are added to it, and rows that no
+ * id names are left alone.  d_out and d_table must not overlap.  n <= 2^30, vocab <= 2^31, dim < 2^31.
+ * `workspace`: pb_embed_backward_workspace bytes (NULL where that is 0), 16-byte aligned, free for other use when
+ * the call's work is done. */
 int64_t pb_embed_backward_workspace(int64_t n, int64_t vocab, int64_t dim);
 int pb_embed_backward(const void* d_out, int32_t dtype, const void* ids, int32_t id_bits, int64_t n, int64_t vocab,
                       int64_t dim, float scale, void* d_table, int32_t table_dtype, int32_t add, void* workspace,
